@@ -394,7 +394,7 @@ def _plain_scan(s):
         carried[:, 1:] = torch.where(done[:, :-1, None] != 0, 0.0, carried[:, 1:])
     # lambda_t = dh_t + keep_t a_{t+1} lambda_{t+1}, from the last step back
     nxt = torch.cat([a[:, 1:], torch.ones_like(a[:, :1])], 1) * keep
-    u = s["dh"].float()
+    u = s["dh"].float().clone()
     u[:, -1] += nxt[:, -1] * s["dh_last"]
     lam = _doubling(nxt.flip(1), u.flip(1)).flip(1)
     dx = lam * na
