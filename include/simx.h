@@ -473,6 +473,187 @@ simx_status simx_adam_step(float* d_params, const float* d_grad, float* d_m, flo
                            const simx_adam_params* params, void* d_workspace,
                            size_t workspace_bytes, void* stream);
 
+/*
+ * Operators of sequence policies: a policy with memory over a rollout, or one that picks from a
+ * large vocabulary.  The paper's agents are multi-layer perceptrons; these are what such a policy
+ * needs beside compute_returns_gae and simx_adam_step.
+ *
+ * Conventions.  Tensors that carry a `dtype` hold fp32 or bf16; parameters, states, statistics and
+ * per-row values are fp32, and every sum, running maximum and state is kept in fp32 or more.  Strides
+ * are in elements, rows are unit-stride along their last axis, and no alignment beyond the
+ * element's is required.  Outputs must not overlap inputs except where it is said.  Calls allocate
+ * nothing, keep nothing between calls and may run on concurrent streams with workspaces of their own
+ * (16-byte aligned, contents irrelevant before and after) and inside captured CUDA graphs.  Results
+ * are the same bits on every run: no sum goes through floating-point atomics.
+ */
+typedef enum simx_dtype { SIMX_F32 = 0, SIMX_BF16 = 1 } simx_dtype;
+
+/* n rows of logits over a vocabulary: row i at i * ld, its gradient at i * grad_ld (grad NULL: none
+   is computed; grad may be logits itself with grad_ld == ld).  pi = softmax(logits / temperature).
+   1 <= vocab < 2^31 - 2^16.  A logit of -inf has probability 0 and gradient 0; a row that has a NaN,
+   +inf, or nothing above -inf gives NaN in its outputs, and so does a token outside the vocabulary. */
+typedef struct simx_logits {
+  const void* logits;
+  void* grad;
+  int64_t ld, grad_ld;
+  int64_t n, vocab;
+  int32_t dtype;
+  float temperature;
+} simx_logits;
+
+/*
+ * Clipped policy loss with a KL and an entropy term, per token, and its gradient with respect to the
+ * logits.  With lp = log pi(action), rho = exp(lp - logp_old) (1 where logp_old is NULL: on-policy,
+ * with the gradient of the log probability) and d = logp_ref - lp:
+ *   L = sum_i w_i ( -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A)
+ *                   + c_kl (exp(d) - d - 1) - c_entropy H[pi] ).
+ * The loss is a sum: a mean over tokens or sequences is a choice of weights (weight NULL: 1 / n).  A
+ * row of weight 0 is not read: its terms, logp and entropy are 0, its gradient row is zeros and its
+ * action may be anything.  adv NULL: no policy term; logp_ref NULL: no KL term.
+ * stats [5] = {L, policy term, sum w (exp(d) - d - 1), sum w H, sum w [clipped]}; clipped: A > 0 and
+ * rho > 1 + clip_high, or A < 0 and rho < 1 - clip_low, where the gradient of the policy term is 0.
+ * logp, entropy [n]: may be NULL.  n == 0: stats are zeros, nothing else is touched.
+ */
+typedef struct simx_token_loss {
+  const int64_t* action;
+  const float* adv;
+  const float* logp_old;
+  const float* logp_ref;
+  const float* weight;
+  float clip_low, clip_high, c_kl, c_entropy;
+  float* logp;
+  float* entropy;
+  float* stats;
+} simx_token_loss;
+size_t simx_token_loss_grad_workspace_size(int64_t n);
+simx_status simx_token_loss_grad(const simx_logits* x, const simx_token_loss* loss, void* d_workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * Preference loss on pairs of sequences (paired log ratios) and its gradient with respect to the
+ * logits.  Sequence q is rows seq_start[q] .. seq_start[q + 1] - 1 (q = 0 .. 2 pairs - 1, possibly
+ * empty; 2p is the preferred one of pair p, 2p + 1 the other).  seq_start ascends within [0, n];
+ * values outside are taken as the nearest bound.
+ *   ratio_q  = sum over its rows with mask != 0 of (log pi(token) - logp_ref),
+ *   margin_p = beta (ratio_2p - ratio_2p+1),
+ *   L = sum_p w_p ( (1 - label_smoothing) softplus(-margin_p) + label_smoothing softplus(margin_p) ).
+ * mask NULL: every row counts; logp_ref NULL: zeros; weight NULL: 1 / pairs.  Rows that are masked or
+ * belong to no sequence are not read, and their gradient rows are zeros.
+ * stats [3] = {L, sum w [margin > 0], sum w margin}; ratio [2 pairs], margin [pairs]: may be NULL.
+ * pairs == 0: stats and every gradient row are zeros.
+ */
+typedef struct simx_preference_loss {
+  const int64_t* token;
+  const int64_t* seq_start;
+  const uint8_t* mask;
+  const float* logp_ref;
+  const float* weight;
+  int64_t pairs;
+  float beta, label_smoothing;
+  float* ratio;
+  float* margin;
+  float* stats;
+} simx_preference_loss;
+size_t simx_preference_loss_grad_workspace_size(int64_t n, int64_t pairs);
+simx_status simx_preference_loss_grad(const simx_logits* x, const simx_preference_loss* loss,
+                                      void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* A [batch][len][channels] tensor: element (b, t, c) at b * sb + t * st + c.  Batch-major sequences,
+   time-major rollouts and slices of a packed projection are all choices of sb and st. */
+typedef struct simx_seq {
+  void* p;
+  int64_t sb, st;
+} simx_seq;
+
+/*
+ * Gated linear recurrence over sequences, per batch entry b and channel c:
+ *   a_t = sigmoid(gate_t + bias_c),  h_t = a_t s_t + (1 - a_t) x_t,
+ *   s_0 = h0 (NULL: zeros),  s_t = done_{t-1} ? 0 : h_{t-1},
+ * as in compute_returns_gae, done_t != 0 ends the episode after step t (whatever h_t holds is then
+ * dropped).  It is evaluated as s_t + (1 - a_t)(x_t - s_t), which keeps long memories exact; a state
+ * that is not finite becomes NaN.  h_last [batch][channels] = the state that the next call continues from (h0 there):
+ * done_{len-1} ? 0 : h_{len-1}, and h0 for len == 0; it is the unrounded state, and it may be h0's own
+ * buffer.  len == 1 is the single-token step of serving.  bias [channels], h0, h_last, done, dh_last,
+ * dbias and dh0 may be NULL.  An empty problem (batch or channels 0) touches nothing.
+ *
+ * simx_gated_scan_grad: given dh (the gradient of h as an output) and dh_last (of h_last; NULL:
+ * zeros), with h as the forward pass saved it,
+ *   lambda_t = dh_t + (done_t ? 0 : t + 1 < len ? a_{t+1} lambda_{t+1} : dh_last),
+ *   dx_t = (1 - a_t) lambda_t,  dgate_t = a_t (1 - a_t) (s_t - x_t) lambda_t,
+ *   dbias = sum over b and t of dgate (before its rounding; zeros for len == 0),  dh0 = a_0 lambda_0
+ *   (dh_last for len == 0).
+ */
+typedef struct simx_scan {
+  int64_t batch, len, channels;
+  int32_t dtype;       /* of x, gate, h, dh, dx, dgate */
+  simx_seq x, gate, h; /* h: output of the forward pass, input of the backward pass */
+  const float* bias;
+  const float* h0;
+  const uint8_t* done; /* element (b, t) at b * done_sb + t * done_st */
+  int64_t done_sb, done_st;
+  float* h_last;       /* forward */
+  simx_seq dh, dx, dgate; /* backward, with what follows */
+  const float* dh_last;
+  float* dbias;
+  float* dh0;
+} simx_scan;
+/* Covers both passes; it is 0 where neither needs one (the workspace may then be NULL). */
+size_t simx_gated_scan_workspace_size(int64_t batch, int64_t len, int64_t channels);
+simx_status simx_gated_scan(const simx_scan* s, void* d_workspace, size_t workspace_bytes, void* stream);
+simx_status simx_gated_scan_grad(const simx_scan* s, void* d_workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/*
+ * Dropout of a branch, its addition to the residual stream, and the root-mean-square norm of the sum:
+ *   z = residual + keep x scale (residual NULL: zeros),  rstd = 1 / sqrt(mean z^2 + eps),
+ *   y = z rstd gain.
+ * rstd and y come from the unrounded z.  z and rstd may be NULL.  z may be x's or residual's own
+ * buffer and y may be x's (with the same ld).
+ * keep is drawn, never stored: element (row, col) of row = row_base + i takes 16-bit field col % 8 of
+ * Philox4x32-10 with key `seed` and counter (col / 8, row, step, 6): word (col % 8) / 2, low half
+ * first.  It is kept where the field is at least thr = round(65536 p), so the drop probability is
+ * thr / 65536, and scale = 65536 / (65536 - thr).  What is dropped counts as 0 even if it is not
+ * finite.  p == 0 draws nothing.  1 <= width <= 16384, n and row_base + n at most 2^32.
+ *
+ * simx_dropout_add_norm_grad: given dy and dz (the gradient that reaches z from the residual stream;
+ * NULL: zeros), with z and rstd as the forward pass saved them, and zh = z rstd:
+ *   dresidual = dz + rstd (dy gain - zh mean(dy gain zh)),  dx = keep scale dresidual,
+ *   dgain = sum over rows of dy zh.
+ * dx, dresidual and dgain may be NULL.  dx may be dy's or dz's own buffer, dresidual likewise (the
+ * other of the two).  n == 0: dgain is zeros, nothing else is touched.
+ */
+typedef struct simx_norm {
+  int64_t n, width;
+  int32_t dtype; /* of x, residual, z, y, dy, dz, dx, dresidual */
+  float p, eps;
+  uint64_t seed;
+  uint32_t step;
+  uint32_t row_base;
+  const float* gain; /* [width] */
+  float* rstd;       /* [n]: output of the forward pass, input of the backward pass */
+  const void* x;
+  int64_t x_ld;
+  const void* residual;
+  int64_t residual_ld;
+  void* z; /* output of the forward pass, input of the backward pass */
+  int64_t z_ld;
+  void* y;
+  int64_t y_ld;
+  const void* dy; /* backward, with what follows */
+  int64_t dy_ld;
+  const void* dz;
+  int64_t dz_ld;
+  void* dx;
+  int64_t dx_ld;
+  void* dresidual;
+  int64_t dresidual_ld;
+  float* dgain;
+} simx_norm;
+simx_status simx_dropout_add_norm(const simx_norm* a, void* stream);
+size_t simx_dropout_add_norm_grad_workspace_size(int64_t n, int64_t width);
+simx_status simx_dropout_add_norm_grad(const simx_norm* a, void* d_workspace, size_t workspace_bytes,
+                                       void* stream);
+
 /* Aggregate counters (synchronises the context's last stream). host_out: host. */
 simx_status sim_stats(simx_ctx* ctx, simx_counters* host_out);
 

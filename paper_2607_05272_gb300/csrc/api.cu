@@ -911,6 +911,249 @@ simx_status ppo_loss_grad_noalloc(const simx_mlp* pol, const simx_rollout* buf,
   return SIMX_OK;
 }
 
+// ---------------------------------------------------------------------------
+// Operators of sequence policies (seq_loss.cu, seq_scan.cu, seq_norm.cu).
+// ---------------------------------------------------------------------------
+static int elem_bytes(int dtype) { return dtype == SIMX_F32 ? 4 : dtype == SIMX_BF16 ? 2 : 0; }
+static bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
+static const int64_t kMaxRows = (int64_t)1 << 40;  // rows, steps: byte offsets stay far within 63 bits
+
+static simx_status check_workspace(const void* p, size_t given, size_t need) {
+  if (need && (!p || given < need || misaligned(p, 16)))
+    return fail(SIMX_EINVAL, "workspace of %zu bytes (16-byte aligned) needed, %zu given", need, given);
+  return SIMX_OK;
+}
+
+static simx_status check_logits(const simx_logits* x) {
+  if (!x) return fail(SIMX_EINVAL, "logits are NULL");
+  const int es = elem_bytes(x->dtype);
+  if (!es) return fail(SIMX_EINVAL, "dtype %d", x->dtype);
+  if (x->n < 0 || x->n > kMaxRows) return fail(SIMX_EINVAL, "%lld rows", (long long)x->n);
+  if (x->vocab < 1 || x->vocab >= ((int64_t)1 << 31) - 65536) return fail(SIMX_EINVAL, "vocab %lld", (long long)x->vocab);
+  if (!(x->temperature > 0.0f) || !std::isfinite(x->temperature) || !std::isfinite((float)(1.0 / x->temperature)))
+    return fail(SIMX_EINVAL, "temperature %g", (double)x->temperature);
+  if (x->n == 0) return SIMX_OK;
+  if (!x->logits) return fail(SIMX_EINVAL, "logits are NULL");
+  if (x->ld < x->vocab || x->ld > kMaxRows || (x->grad && (x->grad_ld < x->vocab || x->grad_ld > kMaxRows)))
+    return fail(SIMX_EINVAL, "row strides %lld, %lld below the vocabulary %lld", (long long)x->ld, (long long)x->grad_ld, (long long)x->vocab);
+  if (x->grad == x->logits && x->grad_ld != x->ld) return fail(SIMX_EINVAL, "a gradient in place needs the logits' row stride");
+  if (misaligned(x->logits, es) || misaligned(x->grad, es)) return fail(SIMX_EINVAL, "logits or grad misaligned");
+  return SIMX_OK;
+}
+
+size_t simx_token_loss_grad_workspace_size(int64_t n) { return n < 0 ? 0 : token_workspace_bytes(n); }
+
+simx_status simx_token_loss_grad(const simx_logits* x, const simx_token_loss* l, void* d_workspace,
+                                 size_t workspace_bytes, void* stream) {
+  simx_status v = check_logits(x);
+  if (v != SIMX_OK) return v;
+  if (!l || !l->stats) return fail(SIMX_EINVAL, "loss arguments and stats are required");
+  if (x->n > 0 && !l->action) return fail(SIMX_EINVAL, "actions are required");
+  if (!(l->clip_low >= 0.0f) || !(l->clip_high >= 0.0f) || !std::isfinite(l->clip_low) || !std::isfinite(l->clip_high))
+    return fail(SIMX_EINVAL, "clip range %g, %g", (double)l->clip_low, (double)l->clip_high);
+  if (!std::isfinite(l->c_kl) || !std::isfinite(l->c_entropy)) return fail(SIMX_EINVAL, "c_kl or c_entropy is not finite");
+  v = check_workspace(d_workspace, workspace_bytes, token_workspace_bytes(x->n));
+  if (v != SIMX_OK) return v;
+  TokenArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.x = x->logits;
+  a.g = x->grad;
+  a.ld = x->ld;
+  a.g_ld = x->grad_ld;
+  a.n = x->n;
+  a.V = x->vocab;
+  a.dtype = x->dtype;
+  a.inv_t = (float)(1.0 / x->temperature);
+  a.k = (float)(1.44269504088896340736 / x->temperature);
+  a.inv_t_lo = (float)(1.0 / x->temperature - (double)a.inv_t);
+  a.dk = (float)((double)a.k / 1.44269504088896340736 - 1.0 / x->temperature);
+  a.action = l->action;
+  a.adv = l->adv;
+  a.logp_old = l->logp_old;
+  a.logp_ref = l->logp_ref;
+  a.weight = l->weight;
+  a.w_all = x->n > 0 ? (float)(1.0 / (double)x->n) : 0.0f;
+  a.lo = 1.0f - l->clip_low;
+  a.hi = 1.0f + l->clip_high;
+  a.c_kl = l->logp_ref ? l->c_kl : 0.0f;
+  a.c_entropy = l->c_entropy;
+  a.logp = l->logp;
+  a.entropy = l->entropy;
+  a.stats = l->stats;
+  cudaError_t e = launch_token_loss(a, d_workspace, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, "token loss launch");
+  return SIMX_OK;
+}
+
+size_t simx_preference_loss_grad_workspace_size(int64_t n, int64_t pairs) {
+  return n < 0 || pairs < 0 || n > kMaxRows || pairs > kMaxRows ? 0 : pref_workspace_bytes(n, pairs);
+}
+
+simx_status simx_preference_loss_grad(const simx_logits* x, const simx_preference_loss* l,
+                                      void* d_workspace, size_t workspace_bytes, void* stream) {
+  simx_status v = check_logits(x);
+  if (v != SIMX_OK) return v;
+  if (!l || !l->stats) return fail(SIMX_EINVAL, "loss arguments and stats are required");
+  if (l->pairs < 0 || l->pairs > kMaxRows) return fail(SIMX_EINVAL, "%lld pairs", (long long)l->pairs);
+  if (l->pairs > 0 && (!l->seq_start || (x->n > 0 && !l->token))) return fail(SIMX_EINVAL, "tokens and sequence starts are required");
+  if (!std::isfinite(l->beta)) return fail(SIMX_EINVAL, "beta is not finite");
+  if (!(l->label_smoothing >= 0.0f) || !(l->label_smoothing <= 1.0f)) return fail(SIMX_EINVAL, "label smoothing %g", (double)l->label_smoothing);
+  v = check_workspace(d_workspace, workspace_bytes, pref_workspace_bytes(x->n, l->pairs));
+  if (v != SIMX_OK) return v;
+  PrefArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.x = x->logits;
+  a.g = x->grad;
+  a.ld = x->ld;
+  a.g_ld = x->grad_ld;
+  a.n = x->n;
+  a.V = x->vocab;
+  a.dtype = x->dtype;
+  a.inv_t = (float)(1.0 / x->temperature);
+  a.k = (float)(1.44269504088896340736 / x->temperature);
+  a.inv_t_lo = (float)(1.0 / x->temperature - (double)a.inv_t);
+  a.dk = (float)((double)a.k / 1.44269504088896340736 - 1.0 / x->temperature);
+  a.token = l->token;
+  a.start = l->seq_start;
+  a.mask = l->mask;
+  a.logp_ref = l->logp_ref;
+  a.weight = l->weight;
+  a.pairs = l->pairs;
+  a.w_all = l->pairs > 0 ? (float)(1.0 / (double)l->pairs) : 0.0f;
+  a.beta = l->beta;
+  a.smoothing = l->label_smoothing;
+  a.ratio = l->ratio;
+  a.margin = l->margin;
+  a.stats = l->stats;
+  cudaError_t e = launch_pref_loss(a, d_workspace, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, "preference loss launch");
+  return SIMX_OK;
+}
+
+// A sequence tensor; outputs must not overlap themselves.
+static simx_status check_seq(const simx_scan* s, const simx_seq& q, const char* name, bool output) {
+  if (!q.p) return fail(SIMX_EINVAL, "%s is NULL", name);
+  if (misaligned(q.p, elem_bytes(s->dtype))) return fail(SIMX_EINVAL, "%s misaligned", name);
+  if (q.sb < 0 || q.st < 0 || q.sb > kMaxRows || q.st > kMaxRows)
+    return fail(SIMX_EINVAL, "strides of %s: %lld, %lld", name, (long long)q.sb, (long long)q.st);
+  if (!output) return SIMX_OK;
+  const double c = (double)s->channels, row = (double)q.st * (double)(s->len - 1) + c,
+               col = (double)q.sb * (double)(s->batch - 1) + c;
+  const bool rows = s->len == 1 || (double)q.st >= c, cols = s->batch == 1 || (double)q.sb >= c;
+  const bool apart = s->len == 1 || s->batch == 1 || (double)q.sb >= row || (double)q.st >= col;
+  if (!rows || !cols || !apart) return fail(SIMX_EINVAL, "%s overlaps itself", name);
+  return SIMX_OK;
+}
+
+static simx_status check_scan(const simx_scan* s) {
+  if (!s) return fail(SIMX_EINVAL, "scan arguments are NULL");
+  if (!elem_bytes(s->dtype)) return fail(SIMX_EINVAL, "dtype %d", s->dtype);
+  const int64_t most = (int64_t)1 << 31;
+  if (s->batch < 0 || s->len < 0 || s->channels < 0 || s->batch > most || s->channels > most || s->len > most ||
+      (double)s->batch * (double)s->channels > 68719476736.0)
+    return fail(SIMX_EINVAL, "batch %lld, len %lld, channels %lld", (long long)s->batch, (long long)s->len, (long long)s->channels);
+  return SIMX_OK;
+}
+
+size_t simx_gated_scan_workspace_size(int64_t batch, int64_t len, int64_t channels) {
+  simx_scan s;
+  std::memset(&s, 0, sizeof(s));
+  s.batch = batch;
+  s.len = len;
+  s.channels = channels;
+  return check_scan(&s) == SIMX_OK ? scan_workspace_bytes(batch, len, channels) : 0;
+}
+
+simx_status simx_gated_scan(const simx_scan* s, void* d_workspace, size_t workspace_bytes, void* stream) {
+  simx_status v = check_scan(s);
+  if (v != SIMX_OK) return v;
+  if (s->batch == 0 || s->channels == 0) return SIMX_OK;
+  if (s->len > 0) {
+    if ((v = check_seq(s, s->x, "x", false)) != SIMX_OK) return v;
+    if ((v = check_seq(s, s->gate, "gate", false)) != SIMX_OK) return v;
+    if ((v = check_seq(s, s->h, "h", true)) != SIMX_OK) return v;
+  }
+  (void)d_workspace;  // the forward pass needs none
+  (void)workspace_bytes;
+  cudaError_t e = launch_scan(*s, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, "scan launch");
+  return SIMX_OK;
+}
+
+simx_status simx_gated_scan_grad(const simx_scan* s, void* d_workspace, size_t workspace_bytes, void* stream) {
+  simx_status v = check_scan(s);
+  if (v != SIMX_OK) return v;
+  if (s->batch == 0 || s->channels == 0) return SIMX_OK;
+  if (s->len > 0) {
+    const struct { const simx_seq* q; const char* name; bool output; } all[] = {
+        {&s->x, "x", false}, {&s->gate, "gate", false}, {&s->h, "h", false}, {&s->dh, "dh", false},
+        {&s->dx, "dx", true}, {&s->dgate, "dgate", true}};
+    for (const auto& t : all)
+      if ((v = check_seq(s, *t.q, t.name, t.output)) != SIMX_OK) return v;
+  }
+  v = check_workspace(d_workspace, workspace_bytes, scan_workspace_bytes(s->batch, s->len, s->channels));
+  if (v != SIMX_OK) return v;
+  cudaError_t e = launch_scan_grad(*s, d_workspace, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, "scan gradient launch");
+  return SIMX_OK;
+}
+
+static simx_status check_rows(const simx_norm* a, const void* p, int64_t ld, const char* name, bool required) {
+  if (!p) return required ? fail(SIMX_EINVAL, "%s is NULL", name) : SIMX_OK;
+  if (misaligned(p, elem_bytes(a->dtype))) return fail(SIMX_EINVAL, "%s misaligned", name);
+  if (ld < a->width || ld > kMaxRows) return fail(SIMX_EINVAL, "row stride %lld of %s below the width %lld", (long long)ld, name, (long long)a->width);
+  return SIMX_OK;
+}
+
+static simx_status check_norm(const simx_norm* a) {
+  if (!a) return fail(SIMX_EINVAL, "norm arguments are NULL");
+  if (!elem_bytes(a->dtype)) return fail(SIMX_EINVAL, "dtype %d", a->dtype);
+  if (a->width < 1 || a->width > kNormMaxWidth) return fail(SIMX_EINVAL, "width %lld outside [1, %d]", (long long)a->width, kNormMaxWidth);
+  if (a->n < 0 || a->n > ((int64_t)1 << 32) - (int64_t)a->row_base)
+    return fail(SIMX_EINVAL, "%lld rows from row %u on", (long long)a->n, a->row_base);
+  if (!(a->p >= 0.0f) || !((double)a->p * 65536.0 + 0.5 < 65536.0)) return fail(SIMX_EINVAL, "drop probability %g", (double)a->p);
+  if (a->n > 0 && !a->gain) return fail(SIMX_EINVAL, "gain is NULL");
+  return SIMX_OK;
+}
+
+simx_status simx_dropout_add_norm(const simx_norm* a, void* stream) {
+  simx_status v = check_norm(a);
+  if (v != SIMX_OK) return v;
+  if (!(a->eps > 0.0f) || !std::isfinite(a->eps)) return fail(SIMX_EINVAL, "eps %g", (double)a->eps);
+  if (a->n == 0) return SIMX_OK;
+  if ((v = check_rows(a, a->x, a->x_ld, "x", true)) != SIMX_OK) return v;
+  if ((v = check_rows(a, a->residual, a->residual_ld, "residual", false)) != SIMX_OK) return v;
+  if ((v = check_rows(a, a->z, a->z_ld, "z", false)) != SIMX_OK) return v;
+  if ((v = check_rows(a, a->y, a->y_ld, "y", true)) != SIMX_OK) return v;
+  cudaError_t e = launch_norm(*a, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, "norm launch");
+  return SIMX_OK;
+}
+
+size_t simx_dropout_add_norm_grad_workspace_size(int64_t n, int64_t width) {
+  return n < 0 || width < 1 || width > kNormMaxWidth ? 0 : norm_grad_workspace_bytes(n, width);
+}
+
+simx_status simx_dropout_add_norm_grad(const simx_norm* a, void* d_workspace, size_t workspace_bytes, void* stream) {
+  simx_status v = check_norm(a);
+  if (v != SIMX_OK) return v;
+  if (a->n > 0) {
+    if (!a->rstd) return fail(SIMX_EINVAL, "rstd is NULL");
+    if ((v = check_rows(a, a->z, a->z_ld, "z", true)) != SIMX_OK) return v;
+    if ((v = check_rows(a, a->dy, a->dy_ld, "dy", true)) != SIMX_OK) return v;
+    if ((v = check_rows(a, a->dz, a->dz_ld, "dz", false)) != SIMX_OK) return v;
+    if ((v = check_rows(a, a->dx, a->dx_ld, "dx", false)) != SIMX_OK) return v;
+    if ((v = check_rows(a, a->dresidual, a->dresidual_ld, "dresidual", false)) != SIMX_OK) return v;
+  }
+  if (a->dgain) {
+    v = check_workspace(d_workspace, workspace_bytes, norm_grad_workspace_bytes(a->n, a->width));
+    if (v != SIMX_OK) return v;
+  }
+  cudaError_t e = launch_norm_grad(*a, d_workspace, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(e, "norm gradient launch");
+  return SIMX_OK;
+}
+
 static simx_status gather_stats(simx_ctx* c, unsigned long long host[9]) {
   cudaSetDevice(c->device);
   cudaError_t e = cudaStreamSynchronize(c->last);

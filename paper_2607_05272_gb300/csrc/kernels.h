@@ -233,4 +233,51 @@ size_t loss_wide_workspace(const LossArgs& a);
 cudaError_t launch_loss_wide(const LossArgs& a, void* ws, size_t ws_bytes, cudaStream_t s);
 cudaError_t launch_loss_grad(const LossArgs& a, void* ws, size_t ws_bytes, cudaStream_t s);
 
+
+// seq_loss.cu
+struct TokenArgs {
+  const void* x;
+  void* g;
+  int64_t ld, g_ld, n, V;
+  int dtype;
+  float inv_t, k;             // 1 / T, log2(e) / T
+  float inv_t_lo, dk;         // 1 / T - inv_t; what rounding k added to 1 / T
+  const int64_t* action;
+  const float *adv, *logp_old, *logp_ref, *weight;
+  float w_all;                // the weight of every row without `weight`
+  float lo, hi, c_kl, c_entropy;
+  float *logp, *entropy, *stats;
+  double* part;               // workspace: {policy, kl, entropy, clipped} of each block
+};
+size_t token_workspace_bytes(int64_t n);
+cudaError_t launch_token_loss(TokenArgs a, void* ws, cudaStream_t s);
+struct PrefArgs {
+  const void* x;
+  void* g;
+  int64_t ld, g_ld, n, V;
+  int dtype;
+  float inv_t, k, inv_t_lo, dk;
+  const int64_t *token, *start;
+  const uint8_t* mask;
+  const float *logp_ref, *weight;
+  float w_all;
+  int64_t pairs;
+  float beta, smoothing;
+  float *ratio, *margin, *stats;
+  float *row_m, *row_is, *row_d;  // workspace, per row: maximum, 1 / sum, log ratio
+  float* coef;                    // workspace, per pair: dL / d log pi of the preferred rows, over T
+  double* part;                   // workspace, per pair: loss, accuracy and margin terms
+};
+size_t pref_workspace_bytes(int64_t n, int64_t pairs);
+cudaError_t launch_pref_loss(PrefArgs a, void* ws, cudaStream_t s);
+// seq_scan.cu
+size_t scan_workspace_bytes(int64_t batch, int64_t len, int64_t channels);
+cudaError_t launch_scan(const simx_scan& a, cudaStream_t s);
+cudaError_t launch_scan_grad(const simx_scan& a, void* ws, cudaStream_t s);
+// seq_norm.cu
+constexpr int kNormMaxWidth = 16384;
+size_t norm_grad_workspace_bytes(int64_t n, int64_t width);
+cudaError_t launch_norm(const simx_norm& a, cudaStream_t s);
+cudaError_t launch_norm_grad(const simx_norm& a, void* ws, cudaStream_t s);
+
 }  // namespace simx

@@ -82,6 +82,50 @@ class Counters(C.Structure):
                 ("decisions", C.c_uint64), ("envs_flagged", C.c_uint32), ("status_or", C.c_uint32)]
 
 
+class Logits(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("grad", C.c_void_p), ("ld", C.c_int64),
+                ("grad_ld", C.c_int64), ("n", C.c_int64), ("vocab", C.c_int64),
+                ("dtype", C.c_int32), ("temperature", C.c_float)]
+
+
+class TokenLoss(C.Structure):
+    _fields_ = [("action", C.c_void_p), ("adv", C.c_void_p), ("logp_old", C.c_void_p),
+                ("logp_ref", C.c_void_p), ("weight", C.c_void_p), ("clip_low", C.c_float),
+                ("clip_high", C.c_float), ("c_kl", C.c_float), ("c_entropy", C.c_float),
+                ("logp", C.c_void_p), ("entropy", C.c_void_p), ("stats", C.c_void_p)]
+
+
+class PreferenceLoss(C.Structure):
+    _fields_ = [("token", C.c_void_p), ("seq_start", C.c_void_p), ("mask", C.c_void_p),
+                ("logp_ref", C.c_void_p), ("weight", C.c_void_p), ("pairs", C.c_int64),
+                ("beta", C.c_float), ("label_smoothing", C.c_float), ("ratio", C.c_void_p),
+                ("margin", C.c_void_p), ("stats", C.c_void_p)]
+
+
+class Seq(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("sb", C.c_int64), ("st", C.c_int64)]
+
+
+class Scan(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("len", C.c_int64), ("channels", C.c_int64),
+                ("dtype", C.c_int32), ("x", Seq), ("gate", Seq), ("h", Seq), ("bias", C.c_void_p),
+                ("h0", C.c_void_p), ("done", C.c_void_p), ("done_sb", C.c_int64),
+                ("done_st", C.c_int64), ("h_last", C.c_void_p), ("dh", Seq), ("dx", Seq),
+                ("dgate", Seq), ("dh_last", C.c_void_p), ("dbias", C.c_void_p),
+                ("dh0", C.c_void_p)]
+
+
+class Norm(C.Structure):
+    _fields_ = [("n", C.c_int64), ("width", C.c_int64), ("dtype", C.c_int32), ("p", C.c_float),
+                ("eps", C.c_float), ("seed", C.c_uint64), ("step", C.c_uint32),
+                ("row_base", C.c_uint32), ("gain", C.c_void_p), ("rstd", C.c_void_p),
+                ("x", C.c_void_p), ("x_ld", C.c_int64), ("residual", C.c_void_p),
+                ("residual_ld", C.c_int64), ("z", C.c_void_p), ("z_ld", C.c_int64),
+                ("y", C.c_void_p), ("y_ld", C.c_int64), ("dy", C.c_void_p), ("dy_ld", C.c_int64),
+                ("dz", C.c_void_p), ("dz_ld", C.c_int64), ("dx", C.c_void_p), ("dx_ld", C.c_int64),
+                ("dresidual", C.c_void_p), ("dresidual_ld", C.c_int64), ("dgain", C.c_void_p)]
+
+
 # (name, restype, argtypes) of every exported function, in header order.
 P, I32, I64, U32, U64, F, SZ = (C.c_void_p, C.c_int32, C.c_int64, C.c_uint32, C.c_uint64,
                                 C.c_float, C.c_size_t)
@@ -110,6 +154,16 @@ SIGNATURES = [
     ("ppo_loss_grad_workspace_size", SZ, [P, I64]),
     ("ppo_loss_grad", C.c_int, [P, P, I64, P, P, P, I64, P, P, P, P, SZ, P]),
     ("ppo_loss_grad_noalloc", C.c_int, [P, P, I64, P, P, P, I64, P, P, P, P]),
+    ("simx_token_loss_grad_workspace_size", SZ, [I64]),
+    ("simx_token_loss_grad", C.c_int, [P, P, P, SZ, P]),
+    ("simx_preference_loss_grad_workspace_size", SZ, [I64, I64]),
+    ("simx_preference_loss_grad", C.c_int, [P, P, P, SZ, P]),
+    ("simx_gated_scan_workspace_size", SZ, [I64, I64, I64]),
+    ("simx_gated_scan", C.c_int, [P, P, SZ, P]),
+    ("simx_gated_scan_grad", C.c_int, [P, P, SZ, P]),
+    ("simx_dropout_add_norm", C.c_int, [P, P]),
+    ("simx_dropout_add_norm_grad_workspace_size", SZ, [I64, I64]),
+    ("simx_dropout_add_norm_grad", C.c_int, [P, P, SZ, P]),
     ("sim_stats", C.c_int, [P, P]),
     ("sim_save", C.c_int, [P, P, U64]),
     ("sim_load", C.c_int, [P, P, U64]),
@@ -467,6 +521,225 @@ def ppo_loss_grad_noalloc(policy: Policy, buf: dict, ret, adv, idx, n: int, algo
     _check(lib().ppo_loss_grad_noalloc(C.byref(policy.c), C.byref(r), r.ld, _ptr(ret), _ptr(adv),
                                        _ptr(idx), n, C.byref(p), _ptr(grad), _ptr(stats),
                                        _stream(stream)))
+
+
+# Operators of sequence policies (include/simx.h has the formulas).  Tensors are fp32 or bf16 and
+# strided as they come, with a last axis of unit stride; per-row values, parameters, states and
+# statistics are contiguous fp32.
+
+def _refuse(msg: str):
+    raise SimxError(EINVAL, msg)
+
+
+def _tensor(t, name: str, shape, like):
+    """A data tensor: `like`'s dtype and device, `shape`, unit stride along the last axis."""
+    if t is None:
+        return None
+    if t.dtype != like.dtype or t.device != like.device or t.shape != shape:
+        _refuse("%s: %s %s on %s expected, got %s %s on %s" % (
+            name, tuple(shape), like.dtype, like.device, tuple(t.shape), t.dtype, t.device))
+    if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():
+        _refuse("%s: the last axis needs unit stride" % name)
+    return t.data_ptr()
+
+
+def _flat(t, name: str, dtype, shape, like):
+    """A contiguous tensor of `dtype` and `shape` on `like`'s device."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != like.device or t.shape != shape or not t.is_contiguous():
+        _refuse("%s: contiguous %s %s on %s expected, got %s %s on %s" % (
+            name, tuple(shape), dtype, like.device, tuple(t.shape), t.dtype, t.device))
+    return t.data_ptr()
+
+
+def _dtype(t, name: str, ndim: int):
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dim() != ndim:
+        _refuse("%s: a tensor of %d axes expected" % (name, ndim))
+    if not t.is_cuda:
+        _refuse("%s: not on a CUDA device" % name)
+    if t.get_device() != torch.cuda.current_device():
+        _refuse("%s: on %s, which is not the current device" % (name, t.device))
+    if t.dtype == torch.float32:
+        return torch, 0
+    if t.dtype == torch.bfloat16:
+        return torch, 1
+    _refuse("%s: float32 or bfloat16 expected, got %s" % (name, t.dtype))
+
+
+def _workspace(ws, like):
+    """(pointer, bytes) of a workspace tensor or None."""
+    if ws is None:
+        return None, 0
+    if ws.device != like.device or not ws.is_contiguous():
+        _refuse("workspace: a contiguous tensor on %s expected" % like.device)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _ld(t) -> int:
+    """Row stride of a [n, width] tensor (a single row has none)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _logits(logits, grad, temperature):
+    torch, dt = _dtype(logits, "logits", 2)
+    x = Logits()
+    x.logits = _tensor(logits, "logits", logits.shape, logits)
+    x.grad = _tensor(grad, "grad", logits.shape, logits)
+    x.ld = _ld(logits)
+    x.grad_ld = _ld(grad) if grad is not None else 0
+    x.n, x.vocab = logits.shape
+    x.dtype, x.temperature = dt, temperature
+    return torch, x
+
+
+def token_loss_grad_workspace_size(n: int) -> int:
+    return lib().simx_token_loss_grad_workspace_size(n)
+
+
+def token_loss_grad(logits, action, adv, stats, workspace, logp_old=None, logp_ref=None,
+                    weight=None, clip_low: float = 0.2, clip_high: float = 0.2, c_kl: float = 0.0,
+                    c_entropy: float = 0.0, temperature: float = 1.0, grad=None, logp=None,
+                    entropy=None, stream=None):
+    """The clipped policy loss with KL and entropy terms from logits [n, vocab], and its gradient
+    with respect to them (simx_token_loss_grad).  action: int64 [n]; adv, logp_old, logp_ref,
+    weight, logp, entropy: fp32 [n] or None; stats: fp32 [5] = loss, policy term, KL, entropy,
+    clipped share; grad: like logits, logits itself, or None."""
+    torch, x = _logits(logits, grad, temperature)
+    n, f = logits.shape[:1], torch.float32
+    a = TokenLoss(_flat(action, "action", torch.int64, n, logits), _flat(adv, "adv", f, n, logits),
+                  _flat(logp_old, "logp_old", f, n, logits),
+                  _flat(logp_ref, "logp_ref", f, n, logits), _flat(weight, "weight", f, n, logits),
+                  clip_low, clip_high, c_kl, c_entropy, _flat(logp, "logp", f, n, logits),
+                  _flat(entropy, "entropy", f, n, logits), _flat(stats, "stats", f, (5,), logits))
+    _check(lib().simx_token_loss_grad(C.byref(x), C.byref(a), *_workspace(workspace, logits),
+                                      _stream(stream)))
+
+
+def preference_loss_grad_workspace_size(n: int, pairs: int) -> int:
+    return lib().simx_preference_loss_grad_workspace_size(n, pairs)
+
+
+def preference_loss_grad(logits, token, seq_start, stats, workspace, logp_ref=None, mask=None,
+                         weight=None, beta: float = 0.1, label_smoothing: float = 0.0,
+                         temperature: float = 1.0, grad=None, ratio=None, margin=None, stream=None):
+    """The preference loss on pairs of sequences from their packed logits [n, vocab], and its
+    gradient with respect to them (simx_preference_loss_grad).  token: int64 [n]; seq_start: int64
+    [2 * pairs + 1] row offsets, the preferred sequence of a pair first; mask: uint8 [n] or None;
+    logp_ref: fp32 [n] or None; weight, margin: fp32 [pairs] or None; ratio: fp32 [2 * pairs] or
+    None; stats: fp32 [3] = loss, share of pairs in the right order, mean margin."""
+    torch, x = _logits(logits, grad, temperature)
+    n, f = logits.shape[:1], torch.float32
+    if seq_start is None or seq_start.dim() != 1 or len(seq_start) % 2 != 1:
+        _refuse("seq_start: 2 * pairs + 1 row offsets expected")
+    pairs = len(seq_start) // 2
+    a = PreferenceLoss(_flat(token, "token", torch.int64, n, logits),
+                       _flat(seq_start, "seq_start", torch.int64, seq_start.shape, logits),
+                       _flat(mask, "mask", torch.uint8, n, logits),
+                       _flat(logp_ref, "logp_ref", f, n, logits),
+                       _flat(weight, "weight", f, (pairs,), logits), pairs, beta, label_smoothing,
+                       _flat(ratio, "ratio", f, (2 * pairs,), logits),
+                       _flat(margin, "margin", f, (pairs,), logits),
+                       _flat(stats, "stats", f, (3,), logits))
+    _check(lib().simx_preference_loss_grad(C.byref(x), C.byref(a), *_workspace(workspace, logits),
+                                           _stream(stream)))
+
+
+def gated_scan_workspace_size(batch: int, length: int, channels: int) -> int:
+    return lib().simx_gated_scan_workspace_size(batch, length, channels)
+
+
+def _scan(x, gate, h, bias, h0, done):
+    torch, dt = _dtype(x, "x", 3)
+    s = Scan()
+    s.batch, s.len, s.channels = x.shape
+    s.dtype = dt
+    for name, t in (("x", x), ("gate", gate), ("h", h)):
+        _seq(s, name, t, x)
+    s.bias = _flat(bias, "bias", torch.float32, x.shape[2:], x)
+    s.h0 = _flat(h0, "h0", torch.float32, (x.shape[0], x.shape[2]), x)
+    if done is not None:
+        if done.dtype != torch.uint8 or done.shape != x.shape[:2] or done.device != x.device:
+            _refuse("done: uint8 %s on %s expected" % (tuple(x.shape[:2]), x.device))
+        s.done = done.data_ptr()
+        s.done_sb, s.done_st = done.stride()
+    return torch, s
+
+
+def _seq(s, name: str, t, like):
+    q = getattr(s, name)
+    q.p = _tensor(t, name, like.shape, like)
+    q.sb, q.st = t.stride()[:2] if t is not None else (0, 0)
+
+
+def gated_scan(x, gate, h, workspace=None, bias=None, h0=None, done=None, h_last=None, stream=None):
+    """h_t = a_t h_{t-1} + (1 - a_t) x_t with a_t = sigmoid(gate_t + bias) over x, gate, h
+    [batch, len, channels] of any batch and time strides (simx_gated_scan).  bias: fp32 [channels];
+    h0, h_last: fp32 [batch, channels] (h_last may be h0: the single-token step of serving); done:
+    uint8 [batch, len], nonzero where the state is not carried on; each of them may be None."""
+    torch, s = _scan(x, gate, h, bias, h0, done)
+    s.h_last = _flat(h_last, "h_last", torch.float32, (x.shape[0], x.shape[2]), x)
+    _check(lib().simx_gated_scan(C.byref(s), *_workspace(workspace, x), _stream(stream)))
+
+
+def gated_scan_grad(x, gate, h, dh, dx, dgate, workspace, bias=None, h0=None, done=None,
+                    dh_last=None, dbias=None, dh0=None, stream=None):
+    """The backward pass of gated_scan (simx_gated_scan_grad): dx, dgate and, where given, dbias
+    and dh0 from dh and dh_last, with h as the forward pass left it."""
+    torch, s = _scan(x, gate, h, bias, h0, done)
+    for name, t in (("dh", dh), ("dx", dx), ("dgate", dgate)):
+        _seq(s, name, t, x)
+    state = (x.shape[0], x.shape[2])
+    s.dh_last = _flat(dh_last, "dh_last", torch.float32, state, x)
+    s.dbias = _flat(dbias, "dbias", torch.float32, x.shape[2:], x)
+    s.dh0 = _flat(dh0, "dh0", torch.float32, state, x)
+    _check(lib().simx_gated_scan_grad(C.byref(s), *_workspace(workspace, x), _stream(stream)))
+
+
+def _norm(like, name: str, gain, rstd, p, seed, step, row_base, rows):
+    torch, dt = _dtype(like, name, 2)
+    a = Norm()
+    a.n, a.width = like.shape
+    a.dtype, a.p = dt, p
+    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= row_base < 1 << 32):
+        _refuse("seed, step or row_base out of range")
+    a.seed, a.step, a.row_base = seed, step, row_base
+    a.gain = _flat(gain, "gain", torch.float32, like.shape[1:], like)
+    a.rstd = _flat(rstd, "rstd", torch.float32, like.shape[:1], like)
+    for key, t in rows:
+        if t is not None:
+            setattr(a, key, _tensor(t, key, like.shape, like))
+            setattr(a, key + "_ld", _ld(t))
+    return torch, a
+
+
+def dropout_add_norm(x, gain, y, residual=None, z=None, rstd=None, p: float = 0.0,
+                     eps: float = 1e-6, seed: int = 0, step: int = 0, row_base: int = 0,
+                     stream=None):
+    """z = residual + dropout_p(x) and y = rms_norm(z) * gain over rows [n, width]
+    (simx_dropout_add_norm).  The mask is a function of (seed, step, row_base + row, column) and is
+    not stored.  gain: fp32 [width]; rstd: fp32 [n] or None, kept for the backward pass."""
+    _, a = _norm(x, "x", gain, rstd, p, seed, step, row_base,
+                 (("x", x), ("residual", residual), ("z", z), ("y", y)))
+    a.eps = eps
+    _check(lib().simx_dropout_add_norm(C.byref(a), _stream(stream)))
+
+
+def dropout_add_norm_grad_workspace_size(n: int, width: int) -> int:
+    return lib().simx_dropout_add_norm_grad_workspace_size(n, width)
+
+
+def dropout_add_norm_grad(z, gain, rstd, dy, dx, workspace, dz=None, dresidual=None, dgain=None,
+                          p: float = 0.0, seed: int = 0, step: int = 0, row_base: int = 0,
+                          stream=None):
+    """The backward pass of dropout_add_norm (simx_dropout_add_norm_grad): dx, dresidual and dgain
+    (each may be None) from dy and dz, with z and rstd as the forward pass left them and the same
+    p, seed, step and row_base."""
+    torch, a = _norm(z, "z", gain, rstd, p, seed, step, row_base,
+                     (("z", z), ("dy", dy), ("dz", dz), ("dx", dx), ("dresidual", dresidual)))
+    a.dgain = _flat(dgain, "dgain", torch.float32, z.shape[1:], z)
+    _check(lib().simx_dropout_add_norm_grad(C.byref(a), *_workspace(workspace, z), _stream(stream)))
 
 
 def fma_probe_sink_floats() -> int:
