@@ -986,7 +986,7 @@ simx_status simx_token_loss_grad(const simx_logits* x, const simx_token_loss* l,
 }
 
 size_t simx_preference_loss_grad_workspace_size(int64_t n, int64_t pairs) {
-  return n < 0 || pairs < 0 || n > kMaxRows || pairs > kMaxRows ? 0 : pref_workspace_bytes(n, pairs);
+  return n < 0 || pairs < 0 || n > kMaxRows || pairs >= (int64_t)1 << 30 ? 0 : pref_workspace_bytes(n, pairs);
 }
 
 simx_status simx_preference_loss_grad(const simx_logits* x, const simx_preference_loss* l,
@@ -994,7 +994,7 @@ simx_status simx_preference_loss_grad(const simx_logits* x, const simx_preferenc
   simx_status v = check_logits(x);
   if (v != SIMX_OK) return v;
   if (!l || !l->stats) return fail(SIMX_EINVAL, "loss arguments and stats are required");
-  if (l->pairs < 0 || l->pairs > kMaxRows) return fail(SIMX_EINVAL, "%lld pairs", (long long)l->pairs);
+  if (l->pairs < 0 || l->pairs >= (int64_t)1 << 30) return fail(SIMX_EINVAL, "%lld pairs", (long long)l->pairs);
   if (l->pairs > 0 && (!l->seq_start || (x->n > 0 && !l->token))) return fail(SIMX_EINVAL, "tokens and sequence starts are required");
   if (!std::isfinite(l->beta)) return fail(SIMX_EINVAL, "beta is not finite");
   if (!(l->label_smoothing >= 0.0f) || !(l->label_smoothing <= 1.0f)) return fail(SIMX_EINVAL, "label smoothing %g", (double)l->label_smoothing);

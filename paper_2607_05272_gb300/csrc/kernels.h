@@ -264,7 +264,8 @@ struct PrefArgs {
   int64_t pairs;
   float beta, smoothing;
   float *ratio, *margin, *stats;
-  float *row_m, *row_is, *row_d;  // workspace, per row: maximum, 1 / sum, log ratio
+  float *row_c, *row_is, *row_d;  // workspace, per row: reference, 1 / sum, log ratio
+  int* row_seq;                   // and its sequence, -1: none, or masked
   float* coef;                    // workspace, per pair: dL / d log pi of the preferred rows, over T
   double* part;                   // workspace, per pair: loss, accuracy and margin terms
 };

@@ -7,6 +7,8 @@
 // row's coefficient c = dL / d log pi(a) and entropy coefficient u = w c_entropy
 //   dL / dx_j = (c (delta_ja - p_j) + u p_j (log p_j + H)) / T.
 // Bound by HBM: a row is read once and its gradient written once; about 10 operations per logit.
+#include <algorithm>
+
 #include "kernels.h"
 #include "seq_common.cuh"
 
@@ -16,8 +18,8 @@ using namespace seq;
 
 namespace {
 
-constexpr int kRowThreads = 256;
-constexpr int kMaxParts = 2432;  // blocks that leave partial sums of the statistics
+constexpr int kRowThreads = 256, kStatThreads = 512;
+constexpr int kMaxParts = 4864;  // blocks that leave partial sums of the statistics
 
 template <class T>
 __device__ __forceinline__ const T* row_of(const void* p, int64_t i, int64_t ld) {
@@ -36,69 +38,84 @@ constexpr float kEx2Short = 5.1e-8f;
 struct LogP {
   float hi, lo;   // log pi(token)
   float logs;     // log s, rounded
-  float mean;     // mean of x - m under pi
+  float H;        // entropy
   __device__ __forceinline__ float value() const { return __fadd_rn(hi, lo); }
   __device__ __forceinline__ float minus(float y) const { return __fadd_rn(__fsub_rn(hi, y), lo); }
 };
-template <class Args>
-__device__ __forceinline__ LogP log_prob(const Args& A, float xa, const Part& P) {
+// a + ae = (x_token - ref) / T, s = sum e^((x - ref) / T), mean = its mean exponent (natural), dmean =
+// the mean of what dk multiplies.
+__device__ __forceinline__ LogP log_prob(float a, float ae, float s, float mean, float dmean, float dk) {
   LogP o;
-  o.mean = __fdiv_rn(P.t, P.s);
-  const int u = __float_as_int(P.s);  // s >= 1, or NaN, or 0 (then x_a - m is NaN)
+  const int u = __float_as_int(s);  // positive, or NaN, or 0 (then a is NaN)
   const int e = (u - 0x3F3504F3) >> 23;
   const float f = __int_as_float(u - (int)((uint32_t)e << 23));  // in [sqrt(1/2), sqrt(2))
   const float eh = __fmul_rn((float)e, kLn2Hi);                  // exact
-  const float fix = __fmaf_rn(-A.dk, o.mean, __fmul_rn(kEx2Short, __fsub_rn(1.0f, rcp(P.s))));
-  const float el = __fadd_rn(__fmaf_rn((float)e, kLn2Lo, __fadd_rn(logf(f), fix)), __fsub_rn(P.s, P.s));
+  const float fix = __fmaf_rn(-dk, dmean, kEx2Short);
+  const float el = __fadd_rn(__fmaf_rn((float)e, kLn2Lo, __fadd_rn(logf(f), fix)), __fsub_rn(s, s));
   o.logs = __fadd_rn(eh, el);
-  const float d = __fsub_rn(xa, P.m);
-  const float a = __fmul_rn(d, A.inv_t);
-  const float ae = __fmaf_rn(d, A.inv_t_lo, __fmaf_rn(d, A.inv_t, -a));
+  o.H = __fsub_rn(o.logs, mean);
   o.hi = __fsub_rn(a, eh);
   const float b = __fsub_rn(o.hi, a);
   const float he = __fsub_rn(__fsub_rn(a, __fsub_rn(o.hi, b)), __fadd_rn(eh, b));
   o.lo = __fsub_rn(fabsf(o.hi) < inf() ? __fadd_rn(he, ae) : 0.0f, el);
   return o;
 }
+// With ref = m, the row's maximum (or another value of the size of its logits).
+template <class Args>
+__device__ __forceinline__ LogP log_prob(const Args& A, float xa, const Part& P) {
+  const float mean = __fdiv_rn(P.t, P.s), d = __fsub_rn(xa, P.m);
+  const float a = __fmul_rn(d, A.inv_t);
+  const float ae = __fmaf_rn(d, A.inv_t_lo, __fmaf_rn(d, A.inv_t, -a));
+  // the largest term is exact
+  return log_prob(a, __fmaf_rn(kEx2Short, rcp(P.s), ae), P.s, __fmul_rn(mean, A.inv_t), mean, A.dk);
+}
 
 // What a row's terms need besides the sums.
 struct RowOut {
   float c, u;       // coefficients of the gradient, both over T
-  float H, logs;
+  float H, logs, lp;
 };
 
-// The terms of a token of weight w: the sums' values in terms[5] (fp64: {policy, kl, entropy,
-// clipped} in 1..4), the gradient's coefficients in the result.
-__device__ RowOut token_terms(const TokenArgs& A, int64_t i, float w, float xa, Part P, double (&terms)[5]) {
+__device__ __forceinline__ void write_row_values(const TokenArgs& A, int64_t i, float lp, float H) {
+  if (A.logp) A.logp[i] = lp;
+  if (A.entropy) A.entropy[i] = H;
+}
+
+// The terms of a token of weight w: {policy, kl, entropy, clipped} are added to `terms` (a thread's sum over
+// its few rows; the blocks' sums are joined in fp64), the gradient's coefficients are the result.
+struct RowIn {
+  float adv, old, ref;
+};
+__device__ __forceinline__ RowIn row_in(const TokenArgs& A, int64_t i) {
+  return RowIn{A.adv ? A.adv[i] : 0.0f, A.logp_old ? A.logp_old[i] : 0.0f, A.logp_ref ? A.logp_ref[i] : 0.0f};
+}
+__device__ __forceinline__ RowOut token_terms(const TokenArgs& A, const RowIn& in, float w, const LogP& l, float (&terms)[4]) {
   RowOut o;
   const float it = A.inv_t;
-  const LogP l = log_prob(A, xa, P);
   o.logs = l.logs;
-  o.H = __fsub_rn(l.logs, __fmul_rn(l.mean, it));
+  o.H = l.H;
   const float lp = l.value();
   float c = 0.0f;
   if (A.adv) {
-    const float adv = A.adv[i];
-    const float rho = A.logp_old ? expf(l.minus(A.logp_old[i])) : (lp == lp ? 1.0f : lp);
-    const float a = __fmul_rn(rho, adv);
-    const float b = __fmul_rn(fminf(fmaxf(rho, A.lo), A.hi), adv);
+    const float rho = A.logp_old ? expf(l.minus(in.old)) : (lp == lp ? 1.0f : lp);
+    const float a = __fmul_rn(rho, in.adv);
+    const float b = __fmul_rn(fminf(fmaxf(rho, A.lo), A.hi), in.adv);
     const bool clipped = b < a;
-    terms[1] += -(double)w * (double)(clipped ? b : a);
-    if (clipped) terms[4] += (double)w;
+    terms[0] = __fmaf_rn(-w, clipped ? b : a, terms[0]);
+    if (clipped) terms[3] = __fadd_rn(terms[3], w);
     c = clipped ? 0.0f : -a;
   }
   if (lp != lp) c = lp;
   if (A.logp_ref) {
-    const float d = -l.minus(A.logp_ref[i]);
+    const float d = -l.minus(in.ref);
     const float em = expm1f(d);
-    terms[2] += (double)w * (double)__fsub_rn(em, d);
+    terms[1] = __fmaf_rn(w, __fsub_rn(em, d), terms[1]);
     c = __fmaf_rn(-A.c_kl, em, c);
   }
-  terms[3] += (double)w * (double)o.H;
+  terms[2] = __fmaf_rn(w, o.H, terms[2]);
   o.c = __fmul_rn(__fmul_rn(c, w), it);
   o.u = __fmul_rn(__fmul_rn(w, A.c_entropy), it);
-  if (A.logp) A.logp[i] = lp;
-  if (A.entropy) A.entropy[i] = o.H;
+  o.lp = lp;
   return o;
 }
 
@@ -106,18 +123,137 @@ __device__ __forceinline__ float weight_of(const TokenArgs& A, int64_t i) {
   return A.weight ? A.weight[i] : A.w_all;
 }
 
-// Maximum and sums of a row by a block, on every thread.  sh: 3 floats per warp.
+constexpr float kLn2 = (float)0.69314718055994530942;
+constexpr float kLn2Rest = (float)(0.69314718055994530942 - (double)(float)0.69314718055994530942);
+constexpr float kFar = -1e30f;  // stands for arg = -inf where it is multiplied: 2^kFar is 0
+
+
 template <class T>
-__device__ Part row_sums_loop(const T* x, int V, float k, float* sh) {
-  const int tid = threadIdx.x, warps = kRowThreads / 32;
+struct VecOf {
+  static constexpr int N = 16 / (int)sizeof(T);
+};
+
+__device__ __forceinline__ void unpack(const uint4& q, float (&v)[4], float) {
+  v[0] = __uint_as_float(q.x);
+  v[1] = __uint_as_float(q.y);
+  v[2] = __uint_as_float(q.z);
+  v[3] = __uint_as_float(q.w);
+}
+__device__ __forceinline__ void unpack(const uint4& q, float (&v)[8], __nv_bfloat16) {
+  const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(u[i] << 16);
+    v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ uint4 pack(const float (&v)[4], float) {
+  return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint4 pack(const float (&v)[8], __nv_bfloat16) {
+  return make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+}
+
+// Elements between the 16-byte boundary at or below p and p.
+template <class T>
+__device__ __forceinline__ int phase_of(const T* p) {
+  return (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+}
+
+// Small vocabularies: G lanes per row, NI logits per lane (logit lane + G i), every lane of the group
+// with the row's terms.
+template <class T, int G, int NI>
+__global__ void __launch_bounds__(kRowThreads) k_token_lanes(TokenArgs A) {
+  __shared__ double sh[kRowThreads / 32][4];
+  pdl_trigger();
+  const int lane = threadIdx.x & (G - 1), V = (int)A.V;
+  const int64_t groups = (int64_t)gridDim.x * (kRowThreads / G);
+  const int64_t rounds = (A.n + groups - 1) / groups;  // the same for every lane: shuffles need all of them
+  float terms[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int64_t q = 0; q < rounds; ++q) {
+    const int64_t i = q * groups + ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) / G;
+    const bool live = i < A.n;
+    const float w = live ? weight_of(A, i) : 0.0f;
+    const bool on = w != 0.0f;
+    const T* x = row_of<T>(A.x, live ? i : 0, A.ld);
+    float r[NI];
+    float m = -inf();
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int e = lane + G * j;
+      r[j] = on && e < V ? widen(x[e]) : -inf();
+    }
+    const int64_t a = on ? A.action[i] : -1;
+    const bool in = a >= 0 && a < A.V;
+    const float xa = in ? widen(x[a]) : nan();
+    const RowIn ri = on ? row_in(A, i) : RowIn{0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < NI; ++j) m = fmaxf(m, r[j]);
+#pragma unroll
+    for (int d = G / 2; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    Part p{m, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < NI; ++j) p.s = __fadd_rn(p.s, part_term(r[j], m, A.k, p.t));
+#pragma unroll
+    for (int d = G / 2; d > 0; d /= 2) {
+      p.s = __fadd_rn(p.s, __shfl_xor_sync(0xffffffffu, p.s, d));
+      p.t = __fadd_rn(p.t, __shfl_xor_sync(0xffffffffu, p.t, d));
+    }
+    if (!live) continue;
+    RowOut o{0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (on) o = token_terms(A, ri, w, log_prob(A, xa, p), terms);
+    if (lane == 0) write_row_values(A, i, o.lp, o.H);
+    if (A.g) {
+      T* g = static_cast<T*>(A.g) + i * A.g_ld;
+      const float is = __fdiv_rn(1.0f, p.s);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const int e = lane + G * j;
+        const float d = __fsub_rn(r[j], p.m);
+        const float pj = __fmul_rn(ex2(__fmul_rn(d, A.k)), is);
+        float f = __fmul_rn(pj, -o.c);
+        if (o.u != 0.0f) {
+          const float lpj = fmaxf(__fmaf_rn(d, A.inv_t, -o.logs), -kMost);
+          f = __fmaf_rn(o.u, __fmul_rn(pj, __fadd_rn(lpj, o.H)), f);
+        }
+        if (e == a) f = __fadd_rn(f, o.c);
+        if (e < V) g[e] = narrow<T>(on ? f : 0.0f);
+      }
+    }
+  }
+  double v[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    v[q] = lane == 0 ? (double)terms[q] : 0.0;
+    for (int d = 16; d > 0; d /= 2) v[q] += __shfl_xor_sync(0xffffffffu, v[q], d);
+  }
+  if ((threadIdx.x & 31) == 0)
+    for (int q = 0; q < 4; ++q) sh[threadIdx.x / 32][q] = v[q];
+  __syncthreads();
+  if (threadIdx.x < 4) {
+    double b = 0.0;
+    for (int k = 0; k < kRowThreads / 32; ++k) b += sh[k][threadIdx.x];
+    A.part[(int64_t)blockIdx.x * 4 + threadIdx.x] = b;
+  }
+}
+
+// Maximum and sums of a row by a block of NT threads, on every thread.  sh: 3 floats per warp.
+template <class T, int NT>
+__device__ __noinline__ Part row_sums_loop(const T* x, int V, float k, float* sh) {
+  const int tid = threadIdx.x, warps = NT / 32;
   float m = -inf();
-  for (int j = tid; j < V; j += kRowThreads) m = fmaxf(m, widen(x[j]));
+  for (int j = tid; j < V; j += NT) m = fmaxf(m, widen(x[j]));
   m = max_lanes(m);
   if ((tid & 31) == 0) sh[tid / 32] = m;
   __syncthreads();
   for (int q = 0; q < warps; ++q) m = fmaxf(m, sh[q]);
   Part p{m, 0.0f, 0.0f};
-  for (int j = tid; j < V; j += kRowThreads) p.s = __fadd_rn(p.s, part_term(widen(x[j]), m, k, p.t));
+  for (int j = tid; j < V; j += NT) p.s = __fadd_rn(p.s, part_term(widen(x[j]), m, k, p.t));
   p.s = sum_lanes(p.s);
   p.t = sum_lanes(p.t);
   if ((tid & 31) == 0) {
@@ -133,63 +269,418 @@ __device__ Part row_sums_loop(const T* x, int V, float k, float* sh) {
   return p;
 }
 
-// Any vocabulary: a block per row, passes for the maximum, the sums and the gradient.
+// One gradient element (without the token's own c) from the row's maximum and sums.
+template <class Args>
+__device__ __forceinline__ float grad_far(float x, const Args& A, const Part& p, const RowOut& o) {
+  const float d = __fsub_rn(x, p.m);
+  const float pj = __fdiv_rn(ex2(__fmul_rn(d, A.k)), p.s);
+  const float lpj = fmaxf(__fmaf_rn(d, A.inv_t, -o.logs), -kMost);  // log p held finite: where it is -inf, p is 0
+  return __fmaf_rn(o.u, __fmul_rn(pj, __fadd_rn(lpj, o.H)), __fmul_rn(pj, -o.c));
+}
+// The gradient of a row from its maximum and sums, by a block of NT threads.
+template <class T, int NT, class Args>
+__device__ __noinline__ void row_grad_loop(const T* x, T* g, int V, const Args& A, const Part& p, const RowOut& o, int64_t a) {
+  for (int j = threadIdx.x; j < V; j += NT) {
+    const float v = grad_far(widen(x[j]), A, p, o);
+    g[j] = narrow<T>(j == a ? __fadd_rn(v, o.c) : v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Rows streamed.  A block per row reads it twice: for the sums, from HBM, and for the gradient, from L2
+// (two rows per SM are 78 MB at 131,072 bf16 logits, of 129).  One pass takes the sums: each thread keeps
+// e = 2^(x k - c) with an integer reference c of its own, raised when a logit passes it, so that sums move
+// to another reference by an exact power of two.  No block waits for another one, which is what a row in
+// a cluster's registers costs: it is the kernel of calls with enough rows to fill the GPU.
+// ---------------------------------------------------------------------------
+constexpr int kChunk = 4;  // vectors per thread and step
+constexpr float kNone = -1e30f;  // reference of a thread that has seen nothing
+
+// 2^d for an integer d <= 0, exactly.
+__device__ __forceinline__ float pow2(float d) {
+  return __int_as_float((127 + (int)fmaxf(d, -127.0f)) << 23);
+}
+
+struct Stream {
+  float c, s, t;  // sums of e = 2^(x k - c) and of e (x k - c)
+  __device__ __forceinline__ void raise(float to) {  // to >= c
+    const float d = __fsub_rn(c, to), f = pow2(d);
+    t = __fmul_rn(f, __fmaf_rn(d, s, t));  // s = 0 while c is kNone
+    s = __fmul_rn(f, s);
+    c = to;
+  }
+  template <int M>
+  __device__ __forceinline__ void add(const float (&x)[M], float k) {
+    float m = x[0];
+#pragma unroll
+    for (int j = 1; j < M; ++j) m = fmaxf(m, x[j]);
+    const float top = __fmul_rn(m, k);
+    if (top > c) raise(ceilf(top));
+    float sa = 0.0f, ta = 0.0f;
+#pragma unroll
+    for (int j = 0; j < M; ++j) {
+      const float arg = __fmaf_rn(x[j], k, -c), e = ex2(arg);
+      sa = __fadd_rn(sa, e);
+      ta = __fmaf_rn(e, arg, ta);
+    }
+    if (ta != ta && sa == sa) {  // logits of -inf: 0 times -inf.  Their terms are 0
+      ta = 0.0f;
+#pragma unroll
+      for (int j = 0; j < M; ++j) {
+        const float arg = __fmaf_rn(x[j], k, -c);
+        ta = __fmaf_rn(ex2(arg), fmaxf(arg, kFar), ta);
+      }
+    }
+    s = __fadd_rn(s, sa);
+    t = __fadd_rn(t, ta);
+  }
+};
+
+// Sums of a row over the block, on every thread, with one reference.  sh: 3 floats per warp.
+template <int NT>
+__device__ __forceinline__ Stream stream_join(Stream v, float* sh) {
+  constexpr int W = NT / 32;
+  const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32;
+  v.raise(max_lanes(v.c));
+  v.s = sum_lanes(v.s);
+  v.t = sum_lanes(v.t);
+  if (lane == 0) {
+    sh[warp] = v.c;
+    sh[W + warp] = v.s;
+    sh[2 * W + warp] = v.t;
+  }
+  __syncthreads();
+  Stream o{kNone, 0.0f, 0.0f};
+  if (lane < W) o = Stream{sh[lane], sh[W + lane], sh[2 * W + lane]};
+  o.raise(max_lanes(o.c));
+  o.s = sum_lanes(o.s);
+  o.t = sum_lanes(o.t);
+  return o;
+}
+
+// One vector that may be partial: -inf where the row has nothing.
 template <class T>
-__global__ void __launch_bounds__(kRowThreads) k_token_loop(TokenArgs A) {
-  __shared__ float sh[3 * kRowThreads / 32];
+__device__ __forceinline__ void load_edge(const T* x, int V, int ph, int v, float (&f)[VecOf<T>::N]) {
+#pragma unroll
+  for (int j = 0; j < VecOf<T>::N; ++j) {
+    const int e = v * VecOf<T>::N - ph + j;
+    f[j] = e >= 0 && e < V ? widen(x[e]) : -inf();
+  }
+}
+
+// A thread's sums over a row: full vectors in steps of kChunk, then the partial ones at both ends.
+template <class T, int NT>
+__device__ __forceinline__ Stream stream_sums(const T* x, int V, float k) {
+  constexpr int N = VecOf<T>::N;
+  const int ph = phase_of(x), tid = threadIdx.x;
+  const uint4* g = reinterpret_cast<const uint4*>(x - ph);
+  const int first = ph ? 1 : 0, last = (ph + V) / N;  // the full vectors
+  Stream v{kNone, 0.0f, 0.0f};
+  int i = first + tid;
+  for (; i + (kChunk - 1) * NT < last; i += kChunk * NT) {
+    uint4 q[kChunk];
+#pragma unroll
+    for (int u = 0; u < kChunk; ++u) q[u] = g[i + u * NT];
+#pragma unroll
+    for (int u = 0; u < kChunk; ++u) {
+      float f[N];
+      unpack(q[u], f, T());
+      v.add(f, k);
+    }
+  }
+  for (; i < last; i += NT) {
+    float f[N];
+    unpack(g[i], f, T());
+    v.add(f, k);
+  }
+  if (tid < 2) {
+    const int edge = tid == 0 ? (ph ? 0 : -1) : (last >= first && (ph + V) % N ? last : -1);
+    if (edge >= 0) {
+      float f[N];
+      load_edge(x, V, ph, edge, f);
+      v.add(f, k);
+    }
+  }
+  return v;
+}
+
+// One gradient element from the row's streamed sums: e (arg ul + ur), or e ur.
+template <bool ENT>
+__device__ __forceinline__ float grad_term(float x, float k, float c, float ul, float ur) {
+  const float arg = __fmaf_rn(x, k, -c);
+  return __fmul_rn(ex2(arg), ENT ? __fmaf_rn(fmaxf(arg, kFar), ul, ur) : ur);
+}
+// Vector v of a gradient row g on the grid of phase ph, in one store if it is whole and g is on it.
+template <class T>
+__device__ __forceinline__ void put_vector(T* g, int ph, int V, int v, bool one, const float (&f)[VecOf<T>::N]) {
+  if (one) {
+    __stcs(reinterpret_cast<uint4*>(g - ph) + v, pack(f, T()));
+  } else {
+#pragma unroll
+    for (int j = 0; j < VecOf<T>::N; ++j) {
+      const int e = v * VecOf<T>::N - ph + j;
+      if (e >= 0 && e < V) g[e] = narrow<T>(f[j]);
+    }
+  }
+}
+// The gradient of a row by a block of NT threads; `add` comes to logit `hot`.
+template <class T, int NT, bool ENT>
+__device__ __forceinline__ void stream_grad(const T* x, T* g, int V, float k, float c, float ul, float ur, int hot, float add) {
+  constexpr int N = VecOf<T>::N;
+  const int ph = phase_of(x), tid = threadIdx.x;
+  const bool same = phase_of(g) == ph;
+  const uint4* from = reinterpret_cast<const uint4*>(x - ph);
+  const int first = ph ? 1 : 0, last = (ph + V) / N, nvec = (ph + V + N - 1) / N;
+  const int hv = hot < 0 ? -1 : (hot + ph) / N, hj = (hot + ph) % N;
+  const auto put = [&](int v, const float (&in)[N], bool whole) {
+    float f[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = grad_term<ENT>(in[j], k, c, ul, ur);
+    if (v == hv) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j == hj) f[j] = __fadd_rn(f[j], add);
+    }
+    put_vector<T>(g, ph, V, v, whole && same, f);
+  };
+  int i = first + tid;
+  for (; i + (kChunk - 1) * NT < last; i += kChunk * NT) {
+    uint4 q[kChunk];
+#pragma unroll
+    for (int u = 0; u < kChunk; ++u) q[u] = __ldcs(from + i + u * NT);
+#pragma unroll
+    for (int u = 0; u < kChunk; ++u) {
+      float f[N];
+      unpack(q[u], f, T());
+      put(i + u * NT, f, true);
+    }
+  }
+  for (; i < last; i += NT) {
+    float f[N];
+    unpack(from[i], f, T());
+    put(i, f, true);
+  }
+  if (tid < 2) {
+    const int edge = tid == 0 ? (ph ? 0 : -1) : (last >= first && last < nvec ? last : -1);
+    if (edge >= 0) {
+      float f[N];
+      load_edge(x, V, ph, edge, f);
+      put(edge, f, false);
+    }
+  }
+}
+
+template <class T, int NT>
+__device__ __forceinline__ void zero_row(T* g, int V) {
+  constexpr int N = VecOf<T>::N;
+  const int tid = threadIdx.x, ph = phase_of(g), first = ph ? 1 : 0, last = (ph + V) / N;
+  uint4* to = reinterpret_cast<uint4*>(g - ph);
+  for (int v = first + tid; v < last; v += NT) __stcs(to + v, make_uint4(0u, 0u, 0u, 0u));
+  const int head = first ? min(V, N - ph) : 0, tail = max(head, last * N - ph);
+  if (tid < head) g[tid] = narrow<T>(0.0f);
+  if (tail + tid < V) g[tail + tid] = narrow<T>(0.0f);
+}
+
+// log pi(token) from streamed sums: (x k - c) ln 2 - log s, the product x k exact in two parts.
+template <class Args>
+__device__ __forceinline__ LogP log_prob(const Args& A, float xa, const Stream& v) {
+  const float ph = __fmul_rn(xa, A.k), pl = __fmaf_rn(xa, A.k, -ph);
+  const float h = __fsub_rn(ph, v.c), b = __fsub_rn(h, ph);
+  const float l = __fadd_rn(__fsub_rn(__fsub_rn(ph, __fsub_rn(h, b)), __fadd_rn(v.c, b)), pl);
+  const float a = __fmul_rn(h, kLn2);
+  float ae = __fmaf_rn(h, kLn2, -a);
+  ae = __fmaf_rn(l, kLn2, __fmaf_rn(h, kLn2Rest, ae));
+  ae = __fmaf_rn(-A.dk, xa, ae);  // x k has k's rounding in it too
+  const float mean = __fdiv_rn(v.t, v.s);
+  return log_prob(a, fabsf(a) < inf() ? ae : 0.0f, v.s, __fmul_rn(mean, kLn2), __fdiv_rn(__fadd_rn(mean, v.c), A.k), A.dk);
+}
+
+// Whether a row's streamed sums hold: not for rows of nothing but -inf or values beyond 1e30 either way,
+// and not where something is not a number; those are gone over again from their maximum.
+__device__ __forceinline__ bool stream_holds(const Stream& v) {
+  return v.s > 0.0f && v.s < inf() && fabsf(v.c) < 1e30f;
+}
+
+template <class T, int NT, bool ENT>
+__global__ void __launch_bounds__(NT, 1024 / NT) k_token_stream(TokenArgs A) {
+  __shared__ float sh[2][3 * NT / 32];
   __shared__ RowOut so;
-  const int tid = threadIdx.x;
-  const int V = (int)A.V;
-  double terms[5] = {0.0, 0.0, 0.0, 0.0, 0.0};
+  pdl_trigger();
+  const int tid = threadIdx.x, V = (int)A.V;
+  float terms[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int64_t i = blockIdx.x; i < A.n; i += gridDim.x) {
     const T* x = row_of<T>(A.x, i, A.ld);
     T* g = A.g ? static_cast<T*>(A.g) + i * A.g_ld : nullptr;
     const float w = weight_of(A, i);
     if (w == 0.0f) {
-      if (g)
-        for (int j = tid; j < V; j += kRowThreads) g[j] = narrow<T>(0.0f);
-      if (tid == 0) {
-        if (A.logp) A.logp[i] = 0.0f;
-        if (A.entropy) A.entropy[i] = 0.0f;
-      }
+      if (g) zero_row<T, NT>(g, V);
+      if (tid == 0) write_row_values(A, i, 0.0f, 0.0f);
       continue;
     }
-    const Part p = row_sums_loop(x, V, A.k, sh);
+    const int64_t a = A.action[i];
+    const bool in = a >= 0 && a < A.V;
+    float xa = nan();
+    RowIn ri{0.0f, 0.0f, 0.0f};
     if (tid == 0) {
-      const int64_t a = A.action[i];
-      const float xa = a >= 0 && a < A.V ? widen(x[a]) : nan();
-      so = token_terms(A, i, w, xa, p, terms);
+      if (in) xa = widen(x[a]);
+      ri = row_in(A, i);
+    }
+    const Stream v = stream_join<NT>(stream_sums<T, NT>(x, V, A.k), sh[0]);
+    const bool holds = stream_holds(v);
+    Part p{0.0f, 0.0f, 0.0f};
+    if (!holds) p = row_sums_loop<T, NT>(x, V, A.k, sh[1]);
+    if (tid == 0) {
+      so = token_terms(A, ri, w, holds ? log_prob(A, xa, v) : log_prob(A, xa, p), terms);
+      write_row_values(A, i, so.lp, so.H);
     }
     __syncthreads();
     if (g) {
       const RowOut o = so;
-      const int64_t a = A.action[i];
-      const float is = __fdiv_rn(1.0f, p.s);
-      for (int j = tid; j < V; j += kRowThreads) {
-        const float d = __fsub_rn(widen(x[j]), p.m);
-        const float e = ex2(__fmul_rn(d, A.k));
-        const float pj = __fmul_rn(e, is);
-        float v = __fmul_rn(pj, -o.c);
-        if (o.u != 0.0f) {  // log p held finite: where it is -inf, p is 0
-          const float lpj = fmaxf(__fmaf_rn(d, A.inv_t, -o.logs), -kMost);
-          v = __fmaf_rn(o.u, __fmul_rn(pj, __fadd_rn(lpj, o.H)), v);
-        }
-        if (j == a) v = __fadd_rn(v, o.c);
-        g[j] = narrow<T>(v);
+      if (holds) {
+        const float is = __fdiv_rn(1.0f, v.s);
+        // ENT: p (u (log p + H) - c) = e (arg ul + ur)
+        const float ul = __fmul_rn(__fmul_rn(o.u, kLn2), is);
+        const float ur = __fmul_rn(ENT ? __fmaf_rn(o.u, __fsub_rn(o.H, o.logs), -o.c) : -o.c, is);
+        stream_grad<T, NT, ENT>(x, g, V, A.k, v.c, ul, ur, in ? (int)a : -1, o.c);
+      } else {
+        row_grad_loop<T, NT>(x, g, V, A, p, o, a);
       }
     }
-    __syncthreads();
   }
   if (tid == 0)
-    for (int q = 1; q < 5; ++q) A.part[(int64_t)blockIdx.x * 4 + q - 1] = terms[q];
+    for (int q = 0; q < 4; ++q) A.part[(int64_t)blockIdx.x * 4 + q] = (double)terms[q];
+}
+
+// ---------------------------------------------------------------------------
+// Few rows of a large vocabulary: a cluster of 8 blocks per row, every block's slice in its threads'
+// registers (64 logits each, 262,144 per cluster), read once; the blocks' sums meet in every block's
+// shared memory.
+// ---------------------------------------------------------------------------
+constexpr int kCluster = 8, kClusterThreads = 512, kPerThread = 64;
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void store_peer(float* slot, uint32_t rank, float v) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tcx::su32(slot)), "r"(rank));
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
+}
+
+template <class T, bool ENT>
+__global__ void __launch_bounds__(kClusterThreads, 1) k_token_cluster(TokenArgs A) {
+  constexpr int NT = kClusterThreads, N = VecOf<T>::N, NV = kPerThread / N;
+  __shared__ float sh[3 * NT / 32];
+  __shared__ float peer[3][kCluster];
+  __shared__ RowOut so;
+  pdl_trigger();
+  const uint32_t rank = cluster_rank();
+  const int tid = threadIdx.x, V = (int)A.V;
+  const int64_t i = blockIdx.x / kCluster;
+  const T* x = row_of<T>(A.x, i, A.ld);
+  T* g = A.g ? static_cast<T*>(A.g) + i * A.g_ld : nullptr;
+  const int ph = phase_of(x), nvec = (ph + V + N - 1) / N, per = (nvec + kCluster - 1) / kCluster;
+  const int first = (int)rank * per, last = min(first + per, nvec);
+  const float w = weight_of(A, i);
+  const bool on = w != 0.0f;  // the same in the whole cluster
+  const auto whole = [&](int v) { return v * N >= ph && v * N - ph + N <= V; };
+  const uint4* from = reinterpret_cast<const uint4*>(x - ph);
+  float r[kPerThread];
+  uint4 q[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int v = first + u * NT + tid;
+    if (on && v < last && whole(v)) q[u] = __ldcs(from + v);
+  }
+  const int64_t a = on ? A.action[i] : -1;
+  const bool in = a >= 0 && a < A.V;
+  float xa = nan();
+  RowIn ri{0.0f, 0.0f, 0.0f};
+  if (tid == 0 && on) {
+    if (in) xa = widen(x[a]);
+    ri = row_in(A, i);
+  }
+  Stream t{kNone, 0.0f, 0.0f};
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int v = first + u * NT + tid;
+    float f[N];
+    if (on && v < last) {
+      if (whole(v)) unpack(q[u], f, T());
+      else load_edge(x, V, ph, v, f);
+      t.add(f, A.k);
+#pragma unroll
+      for (int j = 0; j < N; ++j) r[u * N + j] = f[j];
+    }
+  }
+  t = stream_join<NT>(t, sh);
+  cluster_sync();  // every block runs before another one stores into its shared memory
+  if (tid < kCluster) {
+    store_peer(&peer[0][rank], (uint32_t)tid, t.c);
+    store_peer(&peer[1][rank], (uint32_t)tid, t.s);
+    store_peer(&peer[2][rank], (uint32_t)tid, t.t);
+  }
+  cluster_sync();
+  const int lane = tid & 31;
+  t = Stream{kNone, 0.0f, 0.0f};
+  if (lane < kCluster) t = Stream{peer[0][lane], peer[1][lane], peer[2][lane]};
+  t.raise(max_lanes(t.c));
+  t.s = sum_lanes(t.s);
+  t.t = sum_lanes(t.t);
+  const bool holds = !on || stream_holds(t);
+  Part p{0.0f, 0.0f, 0.0f};
+  if (!holds) {  // every block goes over the whole row, and none writes before all have
+    p = row_sums_loop<T, NT>(x, V, A.k, sh);
+    cluster_sync();
+  }
+  float terms[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (tid == 0) {
+    so = RowOut{0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (on) so = token_terms(A, ri, w, holds ? log_prob(A, xa, t) : log_prob(A, xa, p), terms);
+    if (rank == 0) {
+      write_row_values(A, i, so.lp, so.H);
+      for (int k = 0; k < 4; ++k) A.part[i * 4 + k] = (double)terms[k];
+    }
+  }
+  __syncthreads();
+  if (!g) return;
+  const RowOut o = so;
+  const float is = on && holds ? __fdiv_rn(1.0f, t.s) : 0.0f;
+  const float ul = __fmul_rn(__fmul_rn(o.u, kLn2), is);
+  const float ur = __fmul_rn(ENT ? __fmaf_rn(o.u, __fsub_rn(o.H, o.logs), -o.c) : -o.c, is);
+  const bool same = phase_of(g) == ph;
+  const int hv = in ? ((int)a + ph) / N : -1, hj = in ? ((int)a + ph) % N : 0;
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int v = first + u * NT + tid;
+    if (v >= last) continue;
+    float f[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      f[j] = 0.0f;
+      if (on) f[j] = holds ? grad_term<ENT>(r[u * N + j], A.k, t.c, ul, ur) : grad_far(r[u * N + j], A, p, o);
+    }
+    if (v == hv) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j == hj) f[j] = __fadd_rn(f[j], o.c);
+    }
+    put_vector<T>(g, ph, V, v, same && whole(v), f);
+  }
 }
 
 // The statistics from the blocks' partial sums, in a fixed order.
-__global__ void __launch_bounds__(256) k_token_stats(TokenArgs A, int parts) {
-  __shared__ double sh[8][4];
+__global__ void __launch_bounds__(kStatThreads) k_token_stats(TokenArgs A, int parts) {
+  __shared__ double sh[kStatThreads / 32][4];
   pdl_wait();
   double v[4] = {0.0, 0.0, 0.0, 0.0};
-  for (int b = threadIdx.x; b < parts; b += 256)
+  for (int b = threadIdx.x; b < parts; b += kStatThreads)
     for (int q = 0; q < 4; ++q) v[q] += A.part[(int64_t)b * 4 + q];
   for (int q = 0; q < 4; ++q)
     for (int d = 16; d > 0; d /= 2) v[q] += __shfl_xor_sync(0xffffffffu, v[q], d);
@@ -197,7 +688,7 @@ __global__ void __launch_bounds__(256) k_token_stats(TokenArgs A, int parts) {
     for (int q = 0; q < 4; ++q) sh[threadIdx.x / 32][q] = v[q];
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < 8; ++w)
+    for (int w = 1; w < kStatThreads / 32; ++w)
       for (int q = 0; q < 4; ++q) v[q] += sh[w][q];
     A.stats[0] = (float)(v[0] + (double)A.c_kl * v[1] - (double)A.c_entropy * v[2]);
     for (int q = 0; q < 4; ++q) A.stats[1 + q] = (float)v[q];
@@ -219,24 +710,45 @@ __device__ __forceinline__ int64_t seq_of(const PrefArgs& A, int64_t i) {
   return lo >= 0 && i < A.start[lo + 1] ? lo : -1;
 }
 
-template <class T>
-__global__ void __launch_bounds__(kRowThreads) k_pref_rows(PrefArgs A) {
-  __shared__ float sh[3 * kRowThreads / 32];
-  const int tid = threadIdx.x;
-  const int V = (int)A.V;
+// The sequence of every row, -1 for rows that are masked or in none.
+__global__ void __launch_bounds__(256) k_pref_index(PrefArgs A) {
+  pdl_trigger();
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < A.n; i += stride)
+    A.row_seq[i] = A.mask && !A.mask[i] ? -1 : (int)seq_of(A, i);
+}
+
+// First pass: the log ratio and the sums of every row that counts, streamed as in the token loss.
+// row_is < 0 marks a row whose row_c is its maximum (see stream_holds) instead of the sums' reference.
+template <class T, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) k_pref_rows(PrefArgs A) {
+  __shared__ float sh[2][2][3 * NT / 32];
+  pdl_trigger();
+  pdl_wait();
+  const int tid = threadIdx.x, V = (int)A.V;
+  int turn = 0;
   for (int64_t i = blockIdx.x; i < A.n; i += gridDim.x) {
-    if ((A.mask && !A.mask[i]) || seq_of(A, i) < 0) continue;
+    if (A.row_seq[i] < 0) continue;
     const T* x = row_of<T>(A.x, i, A.ld);
-    const Part p = row_sums_loop(x, V, A.k, sh);
+    float xa = nan(), ref = 0.0f;
     if (tid == 0) {
       const int64_t a = A.token[i];
-      const float xa = a >= 0 && a < A.V ? widen(x[a]) : nan();
-      const LogP l = log_prob(A, xa, p);
-      A.row_m[i] = p.m;
-      A.row_is[i] = __fdiv_rn(1.0f, p.s);
-      A.row_d[i] = A.logp_ref ? l.minus(A.logp_ref[i]) : l.value();
+      if (a >= 0 && a < A.V) xa = widen(x[a]);
+      if (A.logp_ref) ref = A.logp_ref[i];
     }
-    __syncthreads();
+    // tables of both parities: a warp may be in the next row while another still reads this one's
+    float(*mine)[3 * NT / 32] = sh[turn & 1];
+    ++turn;
+    const Stream v = stream_join<NT>(stream_sums<T, NT>(x, V, A.k), mine[0]);
+    const bool holds = stream_holds(v);
+    Part p{0.0f, 0.0f, 0.0f};
+    if (!holds) p = row_sums_loop<T, NT>(x, V, A.k, mine[1]);
+    if (tid == 0) {
+      const LogP l = holds ? log_prob(A, xa, v) : log_prob(A, xa, p);
+      A.row_d[i] = A.logp_ref ? l.minus(ref) : l.value();
+      A.row_c[i] = holds ? v.c : p.m;
+      A.row_is[i] = holds ? __fdiv_rn(1.0f, v.s) : __fdiv_rn(-1.0f, p.s);
+    }
   }
 }
 
@@ -244,13 +756,15 @@ __global__ void __launch_bounds__(kRowThreads) k_pref_rows(PrefArgs A) {
 // coefficient.
 __global__ void __launch_bounds__(256) k_pref_pairs(PrefArgs A) {
   __shared__ double sh[2][8];
+  pdl_trigger();
+  pdl_wait();
   const int tid = threadIdx.x;
   for (int64_t p = blockIdx.x; p < A.pairs; p += gridDim.x) {
     for (int h = 0; h < 2; ++h) {
       const int64_t b = clamp_row(A.start[2 * p + h], A.n), e = clamp_row(A.start[2 * p + h + 1], A.n);
       double v = 0.0;
       for (int64_t i = b + tid; i < e; i += 256)
-        if (!A.mask || A.mask[i]) v += (double)A.row_d[i];
+        if (A.row_seq[i] == 2 * p + h) v += (double)A.row_d[i];
       for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
       if ((tid & 31) == 0) sh[h][tid / 32] = v;
     }
@@ -280,11 +794,13 @@ __global__ void __launch_bounds__(256) k_pref_pairs(PrefArgs A) {
   }
 }
 
-// Second pass: the gradient rows; block 0 also sums the statistics.
-template <class T>
-__global__ void __launch_bounds__(kRowThreads) k_pref_grad(PrefArgs A) {
+// Second pass: the gradient rows, last ones first (those may still be in L2); block 0 also sums the
+// statistics.
+template <class T, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) k_pref_grad(PrefArgs A) {
   const int tid = threadIdx.x;
   const int V = (int)A.V;
+  pdl_wait();
   if (blockIdx.x == 0 && tid < 32) {
     double v[3] = {0.0, 0.0, 0.0};
     for (int64_t p = tid; p < A.pairs; p += 32)
@@ -295,37 +811,95 @@ __global__ void __launch_bounds__(kRowThreads) k_pref_grad(PrefArgs A) {
       for (int q = 0; q < 3; ++q) A.stats[q] = (float)v[q];
   }
   if (!A.g) return;
-  for (int64_t i = blockIdx.x; i < A.n; i += gridDim.x) {
+  for (int64_t i = A.n - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
     T* g = static_cast<T*>(A.g) + i * A.g_ld;
-    const int64_t s = (A.mask && !A.mask[i]) ? -1 : seq_of(A, i);
-    if (s < 0) {
-      for (int j = tid; j < V; j += kRowThreads) g[j] = narrow<T>(0.0f);
+    const int q = A.pairs > 0 ? A.row_seq[i] : -1;
+    if (q < 0) {
+      zero_row<T, NT>(g, V);
       continue;
     }
     const T* x = row_of<T>(A.x, i, A.ld);
-    const float m = A.row_m[i], is = A.row_is[i];
-    const float c = (s & 1) ? -A.coef[s >> 1] : A.coef[s >> 1];
+    const float c = A.row_c[i], is = A.row_is[i];
     const int64_t a = A.token[i];
-    const float bad = a >= 0 && a < A.V ? 0.0f : nan();
-    for (int j = tid; j < V; j += kRowThreads) {
-      const float pj = __fmul_rn(ex2(__fmul_rn(__fsub_rn(widen(x[j]), m), A.k)), is);
-      float v = __fmul_rn(pj, -c);
-      if (j == a) v = __fadd_rn(v, c);
-      g[j] = narrow<T>(__fadd_rn(v, bad));
+    const bool in = a >= 0 && a < A.V;
+    float co = (q & 1) ? -A.coef[q >> 1] : A.coef[q >> 1];
+    if (!in) co = nan();
+    if (is > 0.0f) {
+      stream_grad<T, NT, false>(x, g, V, A.k, c, 0.0f, __fmul_rn(-co, is), in ? (int)a : -1, co);
+    } else {
+      const Part p{c, __fdiv_rn(-1.0f, is), 0.0f};
+      row_grad_loop<T, NT>(x, g, V, A, p, RowOut{co, 0.0f, 0.0f, 0.0f, 0.0f}, a);
     }
   }
 }
 
-int row_blocks(int64_t n) {
-  const int64_t most = (int64_t)sm_count() * 8;
-  const int64_t b = n < most ? n : most;
-  return (int)(b < kMaxParts ? b : kMaxParts);
+// The launches of a token loss call; parts: the partial sums that they leave.
+template <class T>
+cudaError_t token_cluster(const TokenArgs& a, int& parts, cudaStream_t s) {
+  parts = (int)a.n;
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute at[1];
+  lc.gridDim = dim3((unsigned)(parts * kCluster));
+  lc.blockDim = dim3(kClusterThreads);
+  lc.stream = s;
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = kCluster;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = 1;
+  count_launches(1);
+  return a.c_entropy != 0.0f && a.g ? cudaLaunchKernelEx(&lc, k_token_cluster<T, true>, a)
+                                    : cudaLaunchKernelEx(&lc, k_token_cluster<T, false>, a);
 }
 
-template <class T>
-void token_rows(const TokenArgs& a, int blocks, cudaStream_t s) {
-  k_token_loop<T><<<blocks, kRowThreads, 0, s>>>(a);
+template <class T, int NT>
+cudaError_t token_stream(const TokenArgs& a, int& parts, cudaStream_t s) {
+  parts = (int)std::min<int64_t>(std::min<int64_t>(a.n, (int64_t)sm_count() * (1024 / NT)), kMaxParts);
+  if (a.c_entropy != 0.0f && a.g) k_token_stream<T, NT, true><<<parts, NT, 0, s>>>(a);
+  else k_token_stream<T, NT, false><<<parts, NT, 0, s>>>(a);
   count_launches(1);
+  return cudaGetLastError();
+}
+
+template <class T, int G, int NI>
+cudaError_t token_lanes(const TokenArgs& a, int& parts, cudaStream_t s) {
+  const int64_t need = (a.n + kRowThreads / G - 1) / (kRowThreads / G);
+  parts = (int)std::min<int64_t>(std::min<int64_t>(need, (int64_t)sm_count() * 8), kMaxParts);
+  k_token_lanes<T, G, NI><<<parts, kRowThreads, 0, s>>>(a);
+  count_launches(1);
+  return cudaGetLastError();
+}
+
+// Threads per streamed row: 16 vectors each.  More leaves them idle between the row's barriers, fewer
+// leaves the row's latency bare; GB/s of the call on one GB300 at half, this and twice as many threads
+// (4 GB of logits and gradient, bf16): vocabulary 8192: 4460 / 4786 / 4462, 16,384: 4458 / 4920 / 4496,
+// 32,768: 4980 / 5434 / 4732, 65,536: 4955 / 5166 / 4425.
+template <class T>
+int stream_threads(int64_t V) {
+  const int64_t bytes = V * (int64_t)sizeof(T);
+  return bytes <= 8192 ? 32 : bytes <= 16384 ? 64 : bytes <= 32768 ? 128 : bytes <= 65536 ? 256 : 512;
+}
+
+// The kernel by the vocabulary: lane groups with 8 logits a lane, then a warp with 32, then streamed rows;
+// rows of 128 KB and more that are too few to fill the GPU, in clusters (131,072 bf16 logits, 8 rows: 19
+// against 26 us; at 19 rows, more than one wave of clusters, 26 against 25).
+template <class T>
+cudaError_t token_rows(const TokenArgs& a, int& parts, cudaStream_t s) {
+  if (a.V <= 32) return token_lanes<T, 4, 8>(a, parts, s);
+  if (a.V <= 64) return token_lanes<T, 8, 8>(a, parts, s);
+  if (a.V <= 128) return token_lanes<T, 16, 8>(a, parts, s);
+  if (a.V <= 256) return token_lanes<T, 32, 8>(a, parts, s);
+  if (a.V <= 512) return token_lanes<T, 32, 16>(a, parts, s);
+  if (a.V <= 1024) return token_lanes<T, 32, 32>(a, parts, s);
+  const bool fits = a.V <= (int64_t)kCluster * kClusterThreads * kPerThread - 16 * VecOf<T>::N;
+  if (fits && a.V * (int64_t)sizeof(T) >= 131072 && a.n * kCluster * 8 <= (int64_t)sm_count() * 7) return token_cluster<T>(a, parts, s);
+  switch (stream_threads<T>(a.V)) {
+    case 32: return token_stream<T, 32>(a, parts, s);
+    case 64: return token_stream<T, 64>(a, parts, s);
+    case 128: return token_stream<T, 128>(a, parts, s);
+    case 256: return token_stream<T, 256>(a, parts, s);
+    default: return token_stream<T, 512>(a, parts, s);
+  }
 }
 
 size_t round16(size_t b) { return (b + 15) & ~(size_t)15; }
@@ -336,46 +910,94 @@ size_t token_workspace_bytes(int64_t) { return (size_t)kMaxParts * 4 * sizeof(do
 
 cudaError_t launch_token_loss(TokenArgs a, void* ws, cudaStream_t s) {
   a.part = static_cast<double*>(ws);
-  int blocks = 0;
+  int parts = 0;
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute at[1];
+  lc.gridDim = dim3(1);
+  lc.blockDim = dim3(kStatThreads);
+  lc.stream = s;
   if (a.n > 0) {
-    blocks = row_blocks(a.n);
-    if (a.dtype == SIMX_F32) token_rows<float>(a, blocks, s);
-    else token_rows<__nv_bfloat16>(a, blocks, s);
+    const cudaError_t e = a.dtype == SIMX_F32 ? token_rows<float>(a, parts, s) : token_rows<__nv_bfloat16>(a, parts, s);
+    if (e != cudaSuccess) return e;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = 1;
   }
-  k_token_stats<<<1, 256, 0, s>>>(a, blocks);
   count_launches(1);
-  return cudaGetLastError();
+  const cudaError_t e = cudaLaunchKernelEx(&lc, k_token_stats, a, parts);
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 size_t pref_workspace_bytes(int64_t n, int64_t pairs) {
-  return 3 * round16((size_t)n * sizeof(float)) + round16((size_t)pairs * sizeof(float)) +
+  return 4 * round16((size_t)n * sizeof(float)) + round16((size_t)pairs * sizeof(float)) +
          (size_t)pairs * 3 * sizeof(double) + 16;
 }
+
+namespace {
+
+template <class T, int NT>
+cudaError_t pref_rows(const PrefArgs& a, bool grad, cudaStream_t s) {
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  const int64_t most = (int64_t)sm_count() * (1024 / NT);
+  lc.gridDim = dim3((unsigned)std::max<int64_t>(1, grad && !a.g ? 1 : std::min(a.n, grad ? 2 * most : most)));
+  lc.blockDim = dim3(NT);
+  lc.stream = s;
+  lc.attrs = at;
+  lc.numAttrs = 1;
+  count_launches(1);
+  return cudaLaunchKernelEx(&lc, grad ? k_pref_grad<T, NT> : k_pref_rows<T, NT>, a);
+}
+template <class T>
+cudaError_t pref_rows(const PrefArgs& a, bool grad, cudaStream_t s) {
+  switch (stream_threads<T>(a.V)) {
+    case 32: return pref_rows<T, 32>(a, grad, s);
+    case 64: return pref_rows<T, 64>(a, grad, s);
+    case 128: return pref_rows<T, 128>(a, grad, s);
+    case 256: return pref_rows<T, 256>(a, grad, s);
+    default: return pref_rows<T, 512>(a, grad, s);
+  }
+}
+
+}  // namespace
 
 cudaError_t launch_pref_loss(PrefArgs a, void* ws, cudaStream_t s) {
   char* w = static_cast<char*>(ws);
   const size_t rows = round16((size_t)a.n * sizeof(float));
-  a.row_m = reinterpret_cast<float*>(w);
+  a.row_c = reinterpret_cast<float*>(w);
   a.row_is = reinterpret_cast<float*>(w + rows);
   a.row_d = reinterpret_cast<float*>(w + 2 * rows);
-  a.coef = reinterpret_cast<float*>(w + 3 * rows);
-  a.part = reinterpret_cast<double*>(w + 3 * rows + round16((size_t)a.pairs * sizeof(float)));
-  const int blocks = row_blocks(a.n > 0 ? a.n : 1);
-  const bool f32 = a.dtype == SIMX_F32;
-  if (a.n > 0 && a.pairs > 0) {
-    if (f32) k_pref_rows<float><<<blocks, kRowThreads, 0, s>>>(a);
-    else k_pref_rows<__nv_bfloat16><<<blocks, kRowThreads, 0, s>>>(a);
-    count_launches(1);
-  }
+  a.row_seq = reinterpret_cast<int*>(w + 3 * rows);
+  a.coef = reinterpret_cast<float*>(w + 4 * rows);
+  a.part = reinterpret_cast<double*>(w + 4 * rows + round16((size_t)a.pairs * sizeof(float)));
+  const auto pass = [&](bool grad) {
+    return a.dtype == SIMX_F32 ? pref_rows<float>(a, grad, s) : pref_rows<__nv_bfloat16>(a, grad, s);
+  };
+  cudaError_t e = cudaSuccess;
   if (a.pairs > 0) {
     const int64_t most = (int64_t)sm_count() * 8;
-    k_pref_pairs<<<(int)(a.pairs < most ? a.pairs : most), 256, 0, s>>>(a);
+    if (a.n > 0) {
+      k_pref_index<<<(int)std::min<int64_t>((a.n + 255) / 256, most), 256, 0, s>>>(a);
+      count_launches(1);
+      if ((e = pass(false)) != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t lc = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.gridDim = dim3((unsigned)std::min(a.pairs, most));
+    lc.blockDim = dim3(256);
+    lc.stream = s;
+    lc.attrs = at;
+    lc.numAttrs = a.n > 0 ? 1 : 0;
     count_launches(1);
+    if ((e = cudaLaunchKernelEx(&lc, k_pref_pairs, a)) != cudaSuccess) return e;
   }
-  if (f32) k_pref_grad<float><<<blocks, kRowThreads, 0, s>>>(a);
-  else k_pref_grad<__nv_bfloat16><<<blocks, kRowThreads, 0, s>>>(a);
-  count_launches(1);
-  return cudaGetLastError();
+  e = pass(true);
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace simx
