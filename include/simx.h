@@ -508,8 +508,8 @@ typedef struct simx_logits {
  *   L = sum_i w_i ( -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A)
  *                   + c_kl (exp(d) - d - 1) - c_entropy H[pi] ).
  * The loss is a sum: a mean over tokens or sequences is a choice of weights (weight NULL: 1 / n).  A
- * row of weight 0 is not read: its terms, logp and entropy are 0, its gradient row is zeros and its
- * action may be anything.  adv NULL: no policy term; logp_ref NULL: no KL term.
+ * row of weight 0 counts for nothing, whatever its logits and its action hold: its terms, logp and
+ * entropy are 0 and its gradient row is zeros.  adv NULL: no policy term; logp_ref NULL: no KL term.
  * stats [5] = {L, policy term, sum w (exp(d) - d - 1), sum w H, sum w [clipped]}; clipped: A > 0 and
  * rho > 1 + clip_high, or A < 0 and rho < 1 - clip_low, where the gradient of the policy term is 0.
  * logp, entropy [n]: may be NULL.  n == 0: stats are zeros, nothing else is touched.
@@ -538,7 +538,7 @@ simx_status simx_token_loss_grad(const simx_logits* x, const simx_token_loss* lo
  *   margin_p = beta (ratio_2p - ratio_2p+1),
  *   L = sum_p w_p ( (1 - label_smoothing) softplus(-margin_p) + label_smoothing softplus(margin_p) ).
  * mask NULL: every row counts; logp_ref NULL: zeros; weight NULL: 1 / pairs.  Rows that are masked or
- * belong to no sequence are not read, and their gradient rows are zeros.
+ * belong to no sequence count for nothing, whatever they hold, and their gradient rows are zeros.
  * stats [3] = {L, sum w [margin > 0], sum w margin}; ratio [2 pairs], margin [pairs]: may be NULL.
  * pairs == 0: stats and every gradient row are zeros.
  */

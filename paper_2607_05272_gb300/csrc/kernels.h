@@ -247,7 +247,7 @@ struct TokenArgs {
   float w_all;                // the weight of every row without `weight`
   float lo, hi, c_kl, c_entropy;
   float *logp, *entropy, *stats;
-  double* part;               // workspace: {policy, kl, entropy, clipped} of each block
+  float* part;                // workspace: {policy, kl, entropy, clipped} of each block
 };
 size_t token_workspace_bytes(int64_t n);
 cudaError_t launch_token_loss(TokenArgs a, void* ws, cudaStream_t s);

@@ -18,7 +18,7 @@ using namespace seq;
 
 namespace {
 
-constexpr int kRowThreads = 256, kStatThreads = 512;
+constexpr int kRowThreads = 256, kStatThreads = 256;
 constexpr int kMaxParts = 4864;  // blocks that leave partial sums of the statistics
 
 template <class T>
@@ -82,7 +82,7 @@ __device__ __forceinline__ void write_row_values(const TokenArgs& A, int64_t i, 
 }
 
 // The terms of a token of weight w: {policy, kl, entropy, clipped} are added to `terms` (a thread's sum over
-// its few rows; the blocks' sums are joined in fp64), the gradient's coefficients are the result.
+// its few rows; the blocks' sums are joined with their rounding errors kept), the gradient's coefficients are the result.
 struct RowIn {
   float adv, old, ref;
 };
@@ -169,7 +169,7 @@ __device__ __forceinline__ int phase_of(const T* p) {
 // with the row's terms.
 template <class T, int G, int NI>
 __global__ void __launch_bounds__(kRowThreads) k_token_lanes(TokenArgs A) {
-  __shared__ double sh[kRowThreads / 32][4];
+  __shared__ float sh[kRowThreads / 32][4];
   pdl_trigger();
   const int lane = threadIdx.x & (G - 1), V = (int)A.V;
   const int64_t groups = (int64_t)gridDim.x * (kRowThreads / G);
@@ -186,16 +186,24 @@ __global__ void __launch_bounds__(kRowThreads) k_token_lanes(TokenArgs A) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int e = lane + G * j;
-      r[j] = on && e < V ? widen(x[e]) : -inf();
+      r[j] = live && e < V ? widen(x[e]) : -inf();
     }
-    const int64_t a = on ? A.action[i] : -1;
-    const bool in = a >= 0 && a < A.V;
-    const float xa = in ? widen(x[a]) : nan();
-    const RowIn ri = on ? row_in(A, i) : RowIn{0.0f, 0.0f, 0.0f};
+    // everything the row takes is on its way at once, what depends on the weight included
+    const int64_t a = live ? A.action[i] : -1;
+    const RowIn ri = live ? row_in(A, i) : RowIn{0.0f, 0.0f, 0.0f};
+    float xa = 0.0f;
 #pragma unroll
-    for (int j = 0; j < NI; ++j) m = fmaxf(m, r[j]);
+    for (int j = 0; j < NI; ++j) {
+      m = fmaxf(m, r[j]);
+      if (lane + G * j == a) xa = r[j];  // one lane of the group at most, if a < V
+    }
 #pragma unroll
-    for (int d = G / 2; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    for (int d = G / 2; d > 0; d /= 2) {
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+      const float other = __shfl_xor_sync(0xffffffffu, xa, d);
+      xa = other != 0.0f ? other : xa;
+    }
+    if (a < 0 || a >= A.V) xa = nan();
     Part p{m, 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < NI; ++j) p.s = __fadd_rn(p.s, part_term(r[j], m, A.k, p.t));
@@ -226,18 +234,15 @@ __global__ void __launch_bounds__(kRowThreads) k_token_lanes(TokenArgs A) {
       }
     }
   }
-  double v[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    v[q] = lane == 0 ? (double)terms[q] : 0.0;
-    for (int d = 16; d > 0; d /= 2) v[q] += __shfl_xor_sync(0xffffffffu, v[q], d);
+    const float v = sum_lanes(lane == 0 ? terms[q] : 0.0f);
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x / 32][q] = v;
   }
-  if ((threadIdx.x & 31) == 0)
-    for (int q = 0; q < 4; ++q) sh[threadIdx.x / 32][q] = v[q];
   __syncthreads();
   if (threadIdx.x < 4) {
-    double b = 0.0;
-    for (int k = 0; k < kRowThreads / 32; ++k) b += sh[k][threadIdx.x];
+    float b = 0.0f;
+    for (int k = 0; k < kRowThreads / 32; ++k) b = __fadd_rn(b, sh[k][threadIdx.x]);
     A.part[(int64_t)blockIdx.x * 4 + threadIdx.x] = b;
   }
 }
@@ -548,7 +553,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_token_stream(TokenArgs A) {
     }
   }
   if (tid == 0)
-    for (int q = 0; q < 4; ++q) A.part[(int64_t)blockIdx.x * 4 + q] = (double)terms[q];
+    for (int q = 0; q < 4; ++q) A.part[(int64_t)blockIdx.x * 4 + q] = terms[q];
 }
 
 // ---------------------------------------------------------------------------
@@ -645,7 +650,7 @@ __global__ void __launch_bounds__(kClusterThreads, 1) k_token_cluster(TokenArgs 
     if (on) so = token_terms(A, ri, w, holds ? log_prob(A, xa, t) : log_prob(A, xa, p), terms);
     if (rank == 0) {
       write_row_values(A, i, so.lp, so.H);
-      for (int k = 0; k < 4; ++k) A.part[i * 4 + k] = (double)terms[k];
+      for (int k = 0; k < 4; ++k) A.part[i * 4 + k] = terms[k];
     }
   }
   __syncthreads();
@@ -675,23 +680,52 @@ __global__ void __launch_bounds__(kClusterThreads, 1) k_token_cluster(TokenArgs 
   }
 }
 
+// A sum as hi + lo, each addition's rounding error kept (Knuth's two-sum): about 46 bits.  fp64 runs at a
+// sixty-fourth of the fp32 rate here, and these few thousand additions took longer in it than the rows.
+struct Sum2 {
+  float hi, lo;
+  __device__ __forceinline__ void add(float v, float rest) {
+    const float s = __fadd_rn(hi, v), b = __fsub_rn(s, hi);
+    const float e = __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(v, b));
+    hi = s;
+    lo = __fadd_rn(lo, __fadd_rn(e, rest));
+  }
+};
+
 // The statistics from the blocks' partial sums, in a fixed order.
 __global__ void __launch_bounds__(kStatThreads) k_token_stats(TokenArgs A, int parts) {
-  __shared__ double sh[kStatThreads / 32][4];
+  __shared__ Sum2 sh[kStatThreads / 32][4];
   pdl_wait();
-  double v[4] = {0.0, 0.0, 0.0, 0.0};
-  for (int b = threadIdx.x; b < parts; b += kStatThreads)
-    for (int q = 0; q < 4; ++q) v[q] += A.part[(int64_t)b * 4 + q];
+  Sum2 v[4] = {};
+  for (int b = threadIdx.x; b < parts; b += kStatThreads) {
+    const float4 p = reinterpret_cast<const float4*>(A.part)[b];
+    v[0].add(p.x, 0.0f);
+    v[1].add(p.y, 0.0f);
+    v[2].add(p.z, 0.0f);
+    v[3].add(p.w, 0.0f);
+  }
+#pragma unroll
   for (int q = 0; q < 4; ++q)
-    for (int d = 16; d > 0; d /= 2) v[q] += __shfl_xor_sync(0xffffffffu, v[q], d);
+    for (int d = 16; d > 0; d /= 2)
+      v[q].add(__shfl_xor_sync(0xffffffffu, v[q].hi, d), __shfl_xor_sync(0xffffffffu, v[q].lo, d));
   if ((threadIdx.x & 31) == 0)
     for (int q = 0; q < 4; ++q) sh[threadIdx.x / 32][q] = v[q];
   __syncthreads();
+  if (threadIdx.x >= 32) return;
+  float out = 0.0f;
+  const int q = threadIdx.x & 3;
+  Sum2 t = {};
+  for (int w = 0; w < kStatThreads / 32; ++w) t.add(sh[w][q].hi, sh[w][q].lo);
+  out = __fadd_rn(t.hi, t.lo);
+  // L = policy + c_kl kl - c_entropy entropy, from the two-part sums
+  const float kh = __shfl_sync(0xffffffffu, t.hi, 1), kl = __shfl_sync(0xffffffffu, t.lo, 1);
+  const float eh = __shfl_sync(0xffffffffu, t.hi, 2), el = __shfl_sync(0xffffffffu, t.lo, 2);
+  if (threadIdx.x < 4) A.stats[1 + q] = out;
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kStatThreads / 32; ++w)
-      for (int q = 0; q < 4; ++q) v[q] += sh[w][q];
-    A.stats[0] = (float)(v[0] + (double)A.c_kl * v[1] - (double)A.c_entropy * v[2]);
-    for (int q = 0; q < 4; ++q) A.stats[1 + q] = (float)v[q];
+    const float a = __fmul_rn(A.c_kl, kh), b = __fmul_rn(-A.c_entropy, eh);
+    t.add(a, __fmaf_rn(A.c_kl, kl, __fmaf_rn(A.c_kl, kh, -a)));
+    t.add(b, __fmaf_rn(-A.c_entropy, el, __fmaf_rn(-A.c_entropy, eh, -b)));
+    A.stats[0] = __fadd_rn(t.hi, t.lo);
   }
 }
 
@@ -906,10 +940,10 @@ size_t round16(size_t b) { return (b + 15) & ~(size_t)15; }
 
 }  // namespace
 
-size_t token_workspace_bytes(int64_t) { return (size_t)kMaxParts * 4 * sizeof(double); }
+size_t token_workspace_bytes(int64_t) { return (size_t)kMaxParts * 4 * sizeof(float); }
 
 cudaError_t launch_token_loss(TokenArgs a, void* ws, cudaStream_t s) {
-  a.part = static_cast<double*>(ws);
+  a.part = static_cast<float*>(ws);
   int parts = 0;
   cudaLaunchConfig_t lc = {};
   cudaLaunchAttribute at[1];

@@ -220,6 +220,10 @@ def _stream(stream=None):
     if stream is not None:
         return C.c_void_p(stream)
     import torch
+    # the handle alone, where torch gives it: current_stream() builds an object, 2.8 us of a call
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is not None:
+        return C.c_void_p(raw(torch.cuda.current_device()))
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
@@ -531,29 +535,30 @@ def _refuse(msg: str):
     raise SimxError(EINVAL, msg)
 
 
-def _tensor(t, name: str, shape, like):
-    """A data tensor: `like`'s dtype and device, `shape`, unit stride along the last axis."""
+def _tensor(t, name: str, like):
+    """A data tensor: `like`'s dtype, shape and device, unit stride along the last axis."""
     if t is None:
         return None
-    if t.dtype != like.dtype or t.device != like.device or t.shape != shape:
+    if t.dtype is not like.dtype or t.shape != like.shape or t.device != like.device:
         _refuse("%s: %s %s on %s expected, got %s %s on %s" % (
-            name, tuple(shape), like.dtype, like.device, tuple(t.shape), t.dtype, t.device))
+            name, tuple(like.shape), like.dtype, like.device, tuple(t.shape), t.dtype, t.device))
     if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():
         _refuse("%s: the last axis needs unit stride" % name)
     return t.data_ptr()
 
 
-def _flat(t, name: str, dtype, shape, like):
-    """A contiguous tensor of `dtype` and `shape` on `like`'s device."""
+def _flat(t, name: str, dtype, shape, device):
+    """A contiguous tensor of `dtype` and `shape` on `device`."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != like.device or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         _refuse("%s: contiguous %s %s on %s expected, got %s %s on %s" % (
-            name, tuple(shape), dtype, like.device, tuple(t.shape), t.dtype, t.device))
+            name, tuple(shape), dtype, device, tuple(t.shape), t.dtype, t.device))
     return t.data_ptr()
 
 
 def _dtype(t, name: str, ndim: int):
+    """(torch, dtype code, device) of an operator's leading tensor."""
     import torch
     if not isinstance(t, torch.Tensor) or t.dim() != ndim:
         _refuse("%s: a tensor of %d axes expected" % (name, ndim))
@@ -561,19 +566,19 @@ def _dtype(t, name: str, ndim: int):
         _refuse("%s: not on a CUDA device" % name)
     if t.get_device() != torch.cuda.current_device():
         _refuse("%s: on %s, which is not the current device" % (name, t.device))
-    if t.dtype == torch.float32:
-        return torch, 0
-    if t.dtype == torch.bfloat16:
-        return torch, 1
+    if t.dtype is torch.float32:
+        return torch, 0, t.device
+    if t.dtype is torch.bfloat16:
+        return torch, 1, t.device
     _refuse("%s: float32 or bfloat16 expected, got %s" % (name, t.dtype))
 
 
-def _workspace(ws, like):
+def _workspace(ws, device):
     """(pointer, bytes) of a workspace tensor or None."""
     if ws is None:
         return None, 0
-    if ws.device != like.device or not ws.is_contiguous():
-        _refuse("workspace: a contiguous tensor on %s expected" % like.device)
+    if ws.device != device or not ws.is_contiguous():
+        _refuse("workspace: a contiguous tensor on %s expected" % device)
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
@@ -583,15 +588,11 @@ def _ld(t) -> int:
 
 
 def _logits(logits, grad, temperature):
-    torch, dt = _dtype(logits, "logits", 2)
-    x = Logits()
-    x.logits = _tensor(logits, "logits", logits.shape, logits)
-    x.grad = _tensor(grad, "grad", logits.shape, logits)
-    x.ld = _ld(logits)
-    x.grad_ld = _ld(grad) if grad is not None else 0
-    x.n, x.vocab = logits.shape
-    x.dtype, x.temperature = dt, temperature
-    return torch, x
+    torch, dt, dev = _dtype(logits, "logits", 2)
+    n, vocab = logits.shape
+    return torch, dev, n, Logits(_tensor(logits, "logits", logits), _tensor(grad, "grad", logits),
+                                 _ld(logits), _ld(grad) if grad is not None else 0, n, vocab, dt,
+                                 temperature)
 
 
 def token_loss_grad_workspace_size(n: int) -> int:
@@ -606,14 +607,14 @@ def token_loss_grad(logits, action, adv, stats, workspace, logp_old=None, logp_r
     with respect to them (simx_token_loss_grad).  action: int64 [n]; adv, logp_old, logp_ref,
     weight, logp, entropy: fp32 [n] or None; stats: fp32 [5] = loss, policy term, KL, entropy,
     clipped share; grad: like logits, logits itself, or None."""
-    torch, x = _logits(logits, grad, temperature)
-    n, f = logits.shape[:1], torch.float32
-    a = TokenLoss(_flat(action, "action", torch.int64, n, logits), _flat(adv, "adv", f, n, logits),
-                  _flat(logp_old, "logp_old", f, n, logits),
-                  _flat(logp_ref, "logp_ref", f, n, logits), _flat(weight, "weight", f, n, logits),
-                  clip_low, clip_high, c_kl, c_entropy, _flat(logp, "logp", f, n, logits),
-                  _flat(entropy, "entropy", f, n, logits), _flat(stats, "stats", f, (5,), logits))
-    _check(lib().simx_token_loss_grad(C.byref(x), C.byref(a), *_workspace(workspace, logits),
+    torch, dev, n, x = _logits(logits, grad, temperature)
+    n, f = (n,), torch.float32
+    a = TokenLoss(_flat(action, "action", torch.int64, n, dev), _flat(adv, "adv", f, n, dev),
+                  _flat(logp_old, "logp_old", f, n, dev), _flat(logp_ref, "logp_ref", f, n, dev),
+                  _flat(weight, "weight", f, n, dev), clip_low, clip_high, c_kl, c_entropy,
+                  _flat(logp, "logp", f, n, dev), _flat(entropy, "entropy", f, n, dev),
+                  _flat(stats, "stats", f, (5,), dev))
+    _check(lib().simx_token_loss_grad(C.byref(x), C.byref(a), *_workspace(workspace, dev),
                                       _stream(stream)))
 
 
@@ -629,20 +630,19 @@ def preference_loss_grad(logits, token, seq_start, stats, workspace, logp_ref=No
     [2 * pairs + 1] row offsets, the preferred sequence of a pair first; mask: uint8 [n] or None;
     logp_ref: fp32 [n] or None; weight, margin: fp32 [pairs] or None; ratio: fp32 [2 * pairs] or
     None; stats: fp32 [3] = loss, share of pairs in the right order, mean margin."""
-    torch, x = _logits(logits, grad, temperature)
-    n, f = logits.shape[:1], torch.float32
+    torch, dev, n, x = _logits(logits, grad, temperature)
+    n, f = (n,), torch.float32
     if seq_start is None or seq_start.dim() != 1 or len(seq_start) % 2 != 1:
         _refuse("seq_start: 2 * pairs + 1 row offsets expected")
     pairs = len(seq_start) // 2
-    a = PreferenceLoss(_flat(token, "token", torch.int64, n, logits),
-                       _flat(seq_start, "seq_start", torch.int64, seq_start.shape, logits),
-                       _flat(mask, "mask", torch.uint8, n, logits),
-                       _flat(logp_ref, "logp_ref", f, n, logits),
-                       _flat(weight, "weight", f, (pairs,), logits), pairs, beta, label_smoothing,
-                       _flat(ratio, "ratio", f, (2 * pairs,), logits),
-                       _flat(margin, "margin", f, (pairs,), logits),
-                       _flat(stats, "stats", f, (3,), logits))
-    _check(lib().simx_preference_loss_grad(C.byref(x), C.byref(a), *_workspace(workspace, logits),
+    a = PreferenceLoss(_flat(token, "token", torch.int64, n, dev),
+                       _flat(seq_start, "seq_start", torch.int64, seq_start.shape, dev),
+                       _flat(mask, "mask", torch.uint8, n, dev),
+                       _flat(logp_ref, "logp_ref", f, n, dev),
+                       _flat(weight, "weight", f, (pairs,), dev), pairs, beta, label_smoothing,
+                       _flat(ratio, "ratio", f, (2 * pairs,), dev),
+                       _flat(margin, "margin", f, (pairs,), dev), _flat(stats, "stats", f, (3,), dev))
+    _check(lib().simx_preference_loss_grad(C.byref(x), C.byref(a), *_workspace(workspace, dev),
                                            _stream(stream)))
 
 
@@ -650,27 +650,25 @@ def gated_scan_workspace_size(batch: int, length: int, channels: int) -> int:
     return lib().simx_gated_scan_workspace_size(batch, length, channels)
 
 
+def _seq(t, name: str, like):
+    """A Seq of a tensor of `like`'s shape."""
+    p = _tensor(t, name, like)
+    return Seq(p, t.stride(0), t.stride(1)) if t is not None else Seq()
+
+
 def _scan(x, gate, h, bias, h0, done):
-    torch, dt = _dtype(x, "x", 3)
-    s = Scan()
-    s.batch, s.len, s.channels = x.shape
-    s.dtype = dt
-    for name, t in (("x", x), ("gate", gate), ("h", h)):
-        _seq(s, name, t, x)
-    s.bias = _flat(bias, "bias", torch.float32, x.shape[2:], x)
-    s.h0 = _flat(h0, "h0", torch.float32, (x.shape[0], x.shape[2]), x)
+    torch, dt, dev = _dtype(x, "x", 3)
+    b, t, c = x.shape
+    d, dsb, dst = None, 0, 0
     if done is not None:
-        if done.dtype != torch.uint8 or done.shape != x.shape[:2] or done.device != x.device:
-            _refuse("done: uint8 %s on %s expected" % (tuple(x.shape[:2]), x.device))
-        s.done = done.data_ptr()
-        s.done_sb, s.done_st = done.stride()
-    return torch, s
-
-
-def _seq(s, name: str, t, like):
-    q = getattr(s, name)
-    q.p = _tensor(t, name, like.shape, like)
-    q.sb, q.st = t.stride()[:2] if t is not None else (0, 0)
+        if done.dtype is not torch.uint8 or done.shape != (b, t) or done.device != dev:
+            _refuse("done: uint8 %s on %s expected" % ((b, t), dev))
+        d = done.data_ptr()
+        dsb, dst = done.stride()
+    f = torch.float32
+    return f, (b, c), dev, Scan(b, t, c, dt, _seq(x, "x", x), _seq(gate, "gate", x), _seq(h, "h", x),
+                                _flat(bias, "bias", f, (c,), dev), _flat(h0, "h0", f, (b, c), dev),
+                                d, dsb, dst)
 
 
 def gated_scan(x, gate, h, workspace=None, bias=None, h0=None, done=None, h_last=None, stream=None):
@@ -678,40 +676,36 @@ def gated_scan(x, gate, h, workspace=None, bias=None, h0=None, done=None, h_last
     [batch, len, channels] of any batch and time strides (simx_gated_scan).  bias: fp32 [channels];
     h0, h_last: fp32 [batch, channels] (h_last may be h0: the single-token step of serving); done:
     uint8 [batch, len], nonzero where the state is not carried on; each of them may be None."""
-    torch, s = _scan(x, gate, h, bias, h0, done)
-    s.h_last = _flat(h_last, "h_last", torch.float32, (x.shape[0], x.shape[2]), x)
-    _check(lib().simx_gated_scan(C.byref(s), *_workspace(workspace, x), _stream(stream)))
+    f, state, dev, s = _scan(x, gate, h, bias, h0, done)
+    s.h_last = _flat(h_last, "h_last", f, state, dev)
+    _check(lib().simx_gated_scan(C.byref(s), *_workspace(workspace, dev), _stream(stream)))
 
 
 def gated_scan_grad(x, gate, h, dh, dx, dgate, workspace, bias=None, h0=None, done=None,
                     dh_last=None, dbias=None, dh0=None, stream=None):
     """The backward pass of gated_scan (simx_gated_scan_grad): dx, dgate and, where given, dbias
     and dh0 from dh and dh_last, with h as the forward pass left it."""
-    torch, s = _scan(x, gate, h, bias, h0, done)
-    for name, t in (("dh", dh), ("dx", dx), ("dgate", dgate)):
-        _seq(s, name, t, x)
-    state = (x.shape[0], x.shape[2])
-    s.dh_last = _flat(dh_last, "dh_last", torch.float32, state, x)
-    s.dbias = _flat(dbias, "dbias", torch.float32, x.shape[2:], x)
-    s.dh0 = _flat(dh0, "dh0", torch.float32, state, x)
-    _check(lib().simx_gated_scan_grad(C.byref(s), *_workspace(workspace, x), _stream(stream)))
+    f, state, dev, s = _scan(x, gate, h, bias, h0, done)
+    s.dh, s.dx, s.dgate = _seq(dh, "dh", x), _seq(dx, "dx", x), _seq(dgate, "dgate", x)
+    s.dh_last = _flat(dh_last, "dh_last", f, state, dev)
+    s.dbias = _flat(dbias, "dbias", f, state[1:], dev)
+    s.dh0 = _flat(dh0, "dh0", f, state, dev)
+    _check(lib().simx_gated_scan_grad(C.byref(s), *_workspace(workspace, dev), _stream(stream)))
 
 
-def _norm(like, name: str, gain, rstd, p, seed, step, row_base, rows):
-    torch, dt = _dtype(like, name, 2)
-    a = Norm()
-    a.n, a.width = like.shape
-    a.dtype, a.p = dt, p
+def _rows(t, name: str, like):
+    """(pointer, row stride) of a tensor of `like`'s shape."""
+    return (_tensor(t, name, like), _ld(t)) if t is not None else (None, 0)
+
+
+def _norm(like, name: str, gain, rstd, p, eps, seed, step, row_base):
+    torch, dt, dev = _dtype(like, name, 2)
+    n, width = like.shape
     if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= row_base < 1 << 32):
         _refuse("seed, step or row_base out of range")
-    a.seed, a.step, a.row_base = seed, step, row_base
-    a.gain = _flat(gain, "gain", torch.float32, like.shape[1:], like)
-    a.rstd = _flat(rstd, "rstd", torch.float32, like.shape[:1], like)
-    for key, t in rows:
-        if t is not None:
-            setattr(a, key, _tensor(t, key, like.shape, like))
-            setattr(a, key + "_ld", _ld(t))
-    return torch, a
+    f = torch.float32
+    return f, dev, (n, width, dt, p, eps, seed, step, row_base, _flat(gain, "gain", f, (width,), dev),
+                    _flat(rstd, "rstd", f, (n,), dev))
 
 
 def dropout_add_norm(x, gain, y, residual=None, z=None, rstd=None, p: float = 0.0,
@@ -720,9 +714,9 @@ def dropout_add_norm(x, gain, y, residual=None, z=None, rstd=None, p: float = 0.
     """z = residual + dropout_p(x) and y = rms_norm(z) * gain over rows [n, width]
     (simx_dropout_add_norm).  The mask is a function of (seed, step, row_base + row, column) and is
     not stored.  gain: fp32 [width]; rstd: fp32 [n] or None, kept for the backward pass."""
-    _, a = _norm(x, "x", gain, rstd, p, seed, step, row_base,
-                 (("x", x), ("residual", residual), ("z", z), ("y", y)))
-    a.eps = eps
+    _, _, head = _norm(x, "x", gain, rstd, p, eps, seed, step, row_base)
+    a = Norm(*head, *_rows(x, "x", x), *_rows(residual, "residual", x), *_rows(z, "z", x),
+             *_rows(y, "y", x))
     _check(lib().simx_dropout_add_norm(C.byref(a), _stream(stream)))
 
 
@@ -736,10 +730,11 @@ def dropout_add_norm_grad(z, gain, rstd, dy, dx, workspace, dz=None, dresidual=N
     """The backward pass of dropout_add_norm (simx_dropout_add_norm_grad): dx, dresidual and dgain
     (each may be None) from dy and dz, with z and rstd as the forward pass left them and the same
     p, seed, step and row_base."""
-    torch, a = _norm(z, "z", gain, rstd, p, seed, step, row_base,
-                     (("z", z), ("dy", dy), ("dz", dz), ("dx", dx), ("dresidual", dresidual)))
-    a.dgain = _flat(dgain, "dgain", torch.float32, z.shape[1:], z)
-    _check(lib().simx_dropout_add_norm_grad(C.byref(a), *_workspace(workspace, z), _stream(stream)))
+    f, dev, head = _norm(z, "z", gain, rstd, p, 0.0, seed, step, row_base)
+    a = Norm(*head, None, 0, None, 0, *_rows(z, "z", z), None, 0, *_rows(dy, "dy", z),
+             *_rows(dz, "dz", z), *_rows(dx, "dx", z), *_rows(dresidual, "dresidual", z),
+             _flat(dgain, "dgain", f, z.shape[1:], dev))
+    _check(lib().simx_dropout_add_norm_grad(C.byref(a), *_workspace(workspace, dev), _stream(stream)))
 
 
 def fma_probe_sink_floats() -> int:
