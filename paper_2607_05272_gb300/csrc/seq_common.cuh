@@ -10,6 +10,7 @@
 #include <cstdint>
 
 #include "devmath.cuh"
+#include "tc_common.cuh"
 
 namespace simx {
 namespace seq {
@@ -63,6 +64,45 @@ __device__ __forceinline__ float sum_lanes(float v) {
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) v = __fadd_rn(v, __shfl_xor_sync(0xffffffffu, v, d));
   return v;
+}
+
+// Clusters: this block's rank, a barrier of all their threads, and a store of 16 bytes into block `rank`'s
+// shared memory that counts them on a barrier of that block: the data carries its own signal, where a
+// cluster barrier's release would wait for every global store on its way.
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void post_peer(float4* slot, uint64_t* bar, uint32_t rank, float4 v) {
+  uint32_t at, on;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tcx::su32(slot)), "r"(rank));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(on) : "r"(tcx::su32(bar)), "r"(rank));
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(at),
+               "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(on)
+               : "memory");
+}
+constexpr long long kPeerCycles = 2000000000ll;  // a peer's posts take microseconds: a second is a failure
+
+// Asynchronous copies into a thread's own places in shared memory (BYTES 4, 8 or 16).
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  if (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tcx::su32(dst)), "l"(src) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(tcx::su32(dst)), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copy_wait_all() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
 }
 
 // Lets the next kernel of the stream start its preamble; waits for the previous one's results.

@@ -150,11 +150,6 @@ __device__ __forceinline__ void unpack(const uint4& q, float (&v)[8], __nv_bfloa
 __device__ __forceinline__ uint4 pack(const float (&v)[4], float) {
   return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
 }
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 __device__ __forceinline__ uint4 pack(const float (&v)[8], __nv_bfloat16) {
   return make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
 }
@@ -563,15 +558,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_token_stream(TokenArgs A) {
 // ---------------------------------------------------------------------------
 constexpr int kCluster = 8, kClusterThreads = 512, kPerThread = 64;
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+// Stores v at `slot` (this block's shared memory) of block `rank` of the cluster.
 __device__ __forceinline__ void store_peer(float* slot, uint32_t rank, float v) {
   uint32_t a;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tcx::su32(slot)), "r"(rank));

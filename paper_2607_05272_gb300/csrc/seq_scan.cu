@@ -9,8 +9,15 @@
 // A state close to unchanged (a near 1) is where fp32 goes wrong: a_t itself has the absolute error
 // 2^-25, which over 1 / (1 - a) steps of memory is a relative error 2^-25 / (1 - a) of the state (1e-3
 // at gate = 10).  So a_t is never formed on the way: b_t = 1 - a_t = sigmoid(-z) has a small relative
-// error, h_t = s_t + b_t (x_t - s_t) and mu_t = lambda_t - b_t lambda_t, one fma each.
-// Bound by HBM: 2 reads and 1 write per element forward, 4 and 2 backward.
+// error, h_t = s_t + b_t (x_t - s_t), mu_t = lambda_t - b_t lambda_t and the product of a's is
+// P - b_t P, one fma each.
+//
+// Bound by HBM: 2 reads and 1 write per element forward, 4 and 2 backward.  Both directions read each
+// element once: a block holds a tile of steps and channels in registers, joins the steps' maps
+// s -> A s + B across its threads (and, where there are few columns and many steps, across a cluster of
+// blocks that share the steps), and applies the state that comes in to the same registers.
+#include <algorithm>
+
 #include "kernels.h"
 #include "seq_common.cuh"
 
@@ -20,18 +27,18 @@ using namespace seq;
 
 namespace {
 
-// sigmoid(z) and sigmoid(-z), each to relative precision.
+// b = sigmoid(-z) and ab = sigmoid(z) sigmoid(-z), each to relative precision.
 struct Gate {
-  float a, b;
+  float b, ab;
 };
 __device__ __forceinline__ Gate gate_of(float z) {
   const float e = ex2(__fmul_rn(-fabsf(z), kLog2e));
   const float r = rcp(__fadd_rn(1.0f, e));
   const float er = __fmul_rn(e, r);
   Gate g;
-  g.a = z >= 0.0f ? r : er;
   g.b = z >= 0.0f ? er : r;
-  if (z != z) g.a = g.b = z;
+  g.ab = __fmul_rn(er, r);
+  if (z != z) g.b = g.ab = z;
   return g;
 }
 
@@ -39,86 +46,665 @@ template <class T>
 __device__ __forceinline__ T* at(const simx_seq& q, int64_t b, int64_t t, int64_t c) {
   return static_cast<T*>(q.p) + b * q.sb + t * q.st + c;
 }
+__device__ __forceinline__ uint8_t done_byte(const simx_scan& A, int64_t b, int64_t t) {
+  return A.done[b * A.done_sb + t * A.done_st];
+}
+__device__ __forceinline__ bool done_at(const simx_scan& A, int64_t b, int64_t t) { return done_byte(A, b, t) != 0; }
 
+// VEC channels of a tensor at p: one access of VEC elements.
+__device__ __forceinline__ void load_vec(const float* p, float (&v)[4]) {
+  const float4 q = *reinterpret_cast<const float4*>(p);
+  v[0] = q.x;
+  v[1] = q.y;
+  v[2] = q.z;
+  v[3] = q.w;
+}
+__device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&v)[4]) {
+  const uint2 q = *reinterpret_cast<const uint2*>(p);
+  v[0] = __uint_as_float(q.x << 16);
+  v[1] = __uint_as_float(q.x & 0xFFFF0000u);
+  v[2] = __uint_as_float(q.y << 16);
+  v[3] = __uint_as_float(q.y & 0xFFFF0000u);
+}
+template <class T>
+__device__ __forceinline__ void load_vec(const T* p, float (&v)[1]) {
+  v[0] = widen(*p);
+}
+__device__ __forceinline__ void store_vec(float* p, const float (&v)[4]) {
+  __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+}
+__device__ __forceinline__ void store_vec(__nv_bfloat16* p, const float (&v)[4]) {
+  __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3])));
+}
+template <class T>
+__device__ __forceinline__ void store_vec(T* p, const float (&v)[1]) {
+  *p = narrow<T>(v[0]);
+}
+// The same of fp32 rows (bias, states), which have no alignment of their own.
+template <int VEC>
+__device__ __forceinline__ void load_row(const float* p, int64_t off, float (&v)[VEC]) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) v[i] = p ? p[off + i] : 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// Short sequences: a thread per column (VEC channels), through time.  The single-token step.
+// ---------------------------------------------------------------------------
 constexpr int kColThreads = 128;
+constexpr int kColSteps = 8;  // at most; all of a thread's loads are on their way at once
 
-// A thread per column (b, c), through time.
-template <class T>
+template <class T, int VEC>
 __global__ void __launch_bounds__(kColThreads) k_scan_columns(simx_scan A) {
+  const int64_t per = (A.channels + VEC - 1) / VEC, cols = A.batch * per;
   const int64_t col = (int64_t)blockIdx.x * kColThreads + threadIdx.x;
-  if (col >= A.batch * A.channels) return;
-  const int64_t b = col / A.channels, c = col - b * A.channels;
-  const float bias = A.bias ? A.bias[c] : 0.0f;
-  float s = A.h0 ? A.h0[col] : 0.0f;
-  for (int64_t t = 0; t < A.len; ++t) {
-    const Gate g = gate_of(__fadd_rn(widen(*at<const T>(A.gate, b, t, c)), bias));
-    const float h = __fmaf_rn(g.b, __fsub_rn(widen(*at<const T>(A.x, b, t, c)), s), s);
-    *at<T>(A.h, b, t, c) = narrow<T>(h);
-    s = A.done && A.done[b * A.done_sb + t * A.done_st] ? 0.0f : h;
+  if (col >= cols) return;
+  const int64_t b = col / per, c = (col - b * per) * VEC;
+  float bias[VEC], s[VEC], g[kColSteps][VEC], x[kColSteps][VEC];
+  bool end[kColSteps];
+#pragma unroll
+  for (int t = 0; t < kColSteps; ++t) {
+    if (t >= A.len) break;
+    load_vec(at<const T>(A.gate, b, t, c), g[t]);
+    load_vec(at<const T>(A.x, b, t, c), x[t]);
+    end[t] = A.done && done_at(A, b, t);
   }
-  if (A.h_last) A.h_last[col] = s;
+  load_row<VEC>(A.bias, c, bias);
+  load_row<VEC>(A.h0, b * A.channels + c, s);
+#pragma unroll
+  for (int t = 0; t < kColSteps; ++t) {
+    if (t >= A.len) break;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      s[i] = __fmaf_rn(gate_of(__fadd_rn(g[t][i], bias[i])).b, __fsub_rn(x[t][i], s[i]), s[i]);
+    store_vec(at<T>(A.h, b, t, c), s);
+    if (end[t]) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s[i] = 0.0f;
+    }
+  }
+  if (A.h_last) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) A.h_last[b * A.channels + c + i] = s[i];
+  }
+}
+
+template <class T, int VEC>
+__global__ void __launch_bounds__(kColThreads) k_scan_grad_columns(simx_scan A, float* part) {
+  const int64_t per = (A.channels + VEC - 1) / VEC, cols = A.batch * per;
+  const int64_t col = (int64_t)blockIdx.x * kColThreads + threadIdx.x;
+  pdl_trigger();
+  if (col >= cols) return;
+  const int64_t b = col / per, c = (col - b * per) * VEC;
+  float bias[VEC], mu[VEC], db[VEC];
+  load_row<VEC>(A.bias, c, bias);
+  load_row<VEC>(A.dh_last, b * A.channels + c, mu);
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) db[i] = 0.0f;
+  for (int64_t t = A.len - 1; t >= 0; --t) {
+    float g[VEC], x[VEC], dh[VEC], s[VEC], dx[VEC], dg[VEC];
+    load_vec(at<const T>(A.gate, b, t, c), g);
+    load_vec(at<const T>(A.x, b, t, c), x);
+    load_vec(at<const T>(A.dh, b, t, c), dh);
+    if (t == 0) load_row<VEC>(A.h0, b * A.channels + c, s);
+    else load_vec(at<const T>(A.h, b, t - 1, c), s);
+    const bool fresh = t > 0 && A.done && done_at(A, b, t - 1), end = A.done && done_at(A, b, t);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const Gate q = gate_of(__fadd_rn(g[i], bias[i]));
+      const float lam = end ? dh[i] : __fadd_rn(dh[i], mu[i]);
+      dx[i] = __fmul_rn(q.b, lam);
+      dg[i] = __fmul_rn(__fmul_rn(q.ab, __fsub_rn(fresh ? 0.0f : s[i], x[i])), lam);
+      db[i] = __fadd_rn(db[i], dg[i]);
+      mu[i] = __fmaf_rn(-q.b, lam, lam);
+    }
+    store_vec(at<T>(A.dx, b, t, c), dx);
+    store_vec(at<T>(A.dgate, b, t, c), dg);
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    if (A.dh0) A.dh0[b * A.channels + c + i] = mu[i];
+    if (part) part[b * A.channels + c + i] = db[i];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of steps and channels.
+// A thread holds S consecutive steps of VEC channels; LC lanes of a warp take neighbouring channels, its
+// 32 / LC groups of lanes and the block's warps consecutive steps.  Per round a block takes
+// warps * (32 / LC) * S steps, the cluster that many of each of its blocks, in rank order, and then all
+// move on.  A thread's steps are the map s -> A s + B; the maps before it are joined by shuffles within
+// the warp, over a table of the warps' maps, and over a table of the blocks' maps that every block posts
+// to all others.  A = kForget marks a map that does not read s (an episode ended in it): what s holds,
+// infinities included, is then gone.
+// ---------------------------------------------------------------------------
+constexpr float kForget = -1.0f;
+constexpr int kMaxWarps = 8;
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ float apply(float A, float B, float s) {
+  return A < 0.0f ? B : __fmaf_rn(A, s, B);
+}
+// (A, B) after (pA, pB)
+__device__ __forceinline__ void compose(float pA, float pB, float& A, float& B) {
+  B = apply(A, B, pB);
+  A = A < 0.0f || pA < 0.0f ? kForget : __fmul_rn(pA, A);
+}
+
+template <int CLT>
+struct TileShared {
+  float4 peer[2][CLT][2][16];  // [parity][rank][A or B]: 64 channels
+  uint64_t bar[2];
+  float table[2][kMaxWarps][2][64];
+};
+
+// The state that comes into each thread's steps: on entry A, B are its map and carry the state before the
+// round, on return s is the state before its first step and carry that after the round.
+template <int VEC, int CLT>
+__device__ __forceinline__ void tile_states(const float (&A)[VEC], const float (&B)[VEC], float (&carry)[VEC], float (&s)[VEC],
+                                            int lcl, uint32_t rank, uint32_t turn, bool& lost, TileShared<CLT>& sh) {
+  const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32, warps = (int)blockDim.x / 32;
+  const int LC = 1 << lcl, cl = lane & (LC - 1), tg = lane >> lcl, GW = 32 >> lcl, parity = (int)(turn & 1u);
+  float pa[VEC], pb[VEC];  // the maps of the warp's groups before this one
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    float a = A[i], b = B[i];
+    for (int d = 1; d < GW; d *= 2) {
+      const float qa = __shfl_up_sync(0xffffffffu, a, d << lcl), qb = __shfl_up_sync(0xffffffffu, b, d << lcl);
+      if (tg >= d) compose(qa, qb, a, b);
+    }
+    if (tg == GW - 1) {
+      sh.table[parity][warp][0][cl * VEC + i] = a;
+      sh.table[parity][warp][1][cl * VEC + i] = b;
+    }
+    pa[i] = __shfl_up_sync(0xffffffffu, a, LC & 31);
+    pb[i] = __shfl_up_sync(0xffffffffu, b, LC & 31);
+    if (tg == 0) {
+      pa[i] = 1.0f;
+      pb[i] = 0.0f;
+    }
+  }
+  __syncthreads();
+  if (CLT == 1) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) s[i] = carry[i];
+    for (int w = 0; w < warps; ++w) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        if (w == warp) s[i] = carry[i];
+        carry[i] = apply(sh.table[parity][w][0][cl * VEC + i], sh.table[parity][w][1][cl * VEC + i], carry[i]);
+      }
+    }
+  } else {
+    float ta[VEC], tb[VEC], wa[VEC], wb[VEC];  // the block's map, and that of the warps before this one
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      ta[i] = wa[i] = 1.0f;
+      tb[i] = wb[i] = 0.0f;
+    }
+    for (int w = 0; w < warps; ++w) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        if (w == warp) {
+          wa[i] = ta[i];
+          wb[i] = tb[i];
+        }
+        float a = sh.table[parity][w][0][cl * VEC + i], b = sh.table[parity][w][1][cl * VEC + i];
+        compose(ta[i], tb[i], a, b);
+        ta[i] = a;
+        tb[i] = b;
+      }
+    }
+    // Warp w posts to block w of the cluster.  A block may post a round while another still reads the one
+    // before, but not the one after: that takes the other's post of this round.
+    uint64_t* bar = &sh.bar[parity];
+    const uint32_t bytes = (uint32_t)LC * 32u;  // per block that posts, of VEC = 4
+    if (threadIdx.x == 0) tcx::mbar_arrive_expect_tx(bar, bytes * CLT);
+    if (warp < CLT && tg == 0) {
+      post_peer(&sh.peer[parity][rank][0][cl], bar, (uint32_t)warp, make_float4(ta[0], ta[1 % VEC], ta[2 % VEC], ta[3 % VEC]));
+      post_peer(&sh.peer[parity][rank][1][cl], bar, (uint32_t)warp, make_float4(tb[0], tb[1 % VEC], tb[2 % VEC], tb[3 % VEC]));
+    }
+    lost = lost || !tcx::mbar_wait(bar, (turn >> 1) & 1u, kPeerCycles);
+#pragma unroll
+    for (int r = 0; r < CLT; ++r) {
+      const float4 a = sh.peer[parity][r][0][cl], b = sh.peer[parity][r][1][cl];
+      const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        if (r == (int)rank) s[i] = apply(wa[i], wb[i], carry[i]);
+        carry[i] = apply(av[i], bv[i], carry[i]);
+      }
+    }
+    if (lost) {  // a post that never came: what the cluster still computes is NaN
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s[i] = carry[i] = nan();
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) s[i] = apply(pa[i], pb[i], s[i]);
+}
+
+// Elements of K tensors on their way: VEC = 4 in the thread's places in shared memory, VEC = 1 in
+// registers.
+template <class T, int VEC, int K, int S>
+struct Ahead {
+  T reg[VEC == 1 ? K * S : 1];
+  T* slot;  // [K * S][threads][VEC]
+  __device__ __forceinline__ void bring(int k, int s, const T* p) {
+    if (VEC == 1) reg[(k * S + s) % (VEC == 1 ? K * S : 1)] = *p;
+    else copy_async<VEC * (int)sizeof(T) < 4 ? 4 : VEC * (int)sizeof(T)>(slot + ((int64_t)(k * S + s) * blockDim.x + threadIdx.x) * VEC, p);
+  }
+  __device__ __forceinline__ void take(int k, int s, float (&v)[VEC]) const {
+    if (VEC == 1) v[0] = widen(reg[(k * S + s) % (VEC == 1 ? K * S : 1)]);
+    else load_vec(slot + ((int64_t)(k * S + s) * blockDim.x + threadIdx.x) * VEC, v);
+  }
+};
+
+constexpr int kTileSteps = 8;
+
+template <class T, int VEC, bool DONE, int CLT>
+__global__ void __launch_bounds__(256, 2) k_scan_tiles(simx_scan A, int lcl, int64_t tiles) {
+  constexpr int S = kTileSteps;
+  extern __shared__ uint4 slots[];
+  __shared__ TileShared<CLT> sh;
+  const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32;
+  const int LC = 1 << lcl, cl = lane & (LC - 1), group = warp * (32 >> lcl) + (lane >> lcl);
+  const int TB = (int)(blockDim.x >> lcl) * S;  // steps per block and round
+  const uint32_t rank = CLT == 1 ? 0u : cluster_rank();
+  if (CLT > 1) {  // every block runs, its barriers ready, before another one posts to it
+    if (threadIdx.x < 2) tcx::mbar_init(&sh.bar[threadIdx.x], 1);
+    tcx::mbar_fence_init();
+    cluster_sync();
+  }
+  const int64_t per = (A.channels + LC * VEC - 1) / (LC * VEC);
+  const int64_t rounds = (A.len + (int64_t)CLT * TB - 1) / ((int64_t)CLT * TB);
+  Ahead<T, VEC, 2, S> in;
+  in.slot = reinterpret_cast<T*>(slots);
+  uint32_t turn = 0;
+  bool lost = false;
+  for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
+    const int64_t b = tile / per, c = ((tile - b * per) * LC + cl) * VEC;
+    const bool mine = c < A.channels;
+    const T* gate = at<const T>(A.gate, b, 0, c);
+    const T* x = at<const T>(A.x, b, 0, c);
+    T* h = at<T>(A.h, b, 0, c);
+    uint8_t next[S] = {};  // of the round to come: whether the state before a step is dropped
+    const auto bring = [&](int64_t t0) {
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const int64_t t = t0 + s;
+        if (t < A.len && mine) {
+          in.bring(0, s, gate + t * A.gate.st);
+          in.bring(1, s, x + t * A.x.st);
+        }
+        if (DONE) next[s] = t > 0 && t < A.len ? done_byte(A, b, t - 1) : (uint8_t)0;
+      }
+      if (VEC > 1) copy_commit();
+    };
+    int64_t t0 = (int64_t)rank * TB + group * S;
+    bring(t0);
+    float bias[VEC], carry[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) bias[i] = carry[i] = 0.0f;
+    if (mine) {
+      load_row<VEC>(A.bias, c, bias);
+      load_row<VEC>(A.h0, b * A.channels + c, carry);
+    }
+    for (int64_t round = 0; round < rounds; ++round, t0 += (int64_t)CLT * TB) {
+      float bt[S][VEC], xt[S][VEC], a[VEC], s[VEC], st[VEC];
+      if (VEC > 1) copy_wait_all();
+      uint32_t resets = 0;
+      if (DONE) {
+#pragma unroll
+        for (int k = 0; k < S; ++k) resets |= (uint32_t)(next[k] != 0) << k;
+      }
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        const bool live = mine && t0 + k < A.len;
+        float g[VEC];
+        in.take(0, k, g);
+        in.take(1, k, xt[k]);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          bt[k][i] = live ? gate_of(__fadd_rn(g[i], bias[i])).b : 0.0f;  // past the end: the state stays
+          if (!live) xt[k][i] = 0.0f;
+        }
+      }
+      if (round + 1 < rounds) bring(t0 + (int64_t)CLT * TB);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        a[i] = 1.0f;
+        s[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < S; ++k) {
+          if (DONE && (resets >> k & 1u)) s[i] = 0.0f;
+          s[i] = __fmaf_rn(bt[k][i], __fsub_rn(xt[k][i], s[i]), s[i]);
+          a[i] = __fmaf_rn(-bt[k][i], a[i], a[i]);
+        }
+        if (DONE && resets) a[i] = kForget;
+      }
+      tile_states<VEC, CLT>(a, s, carry, st, lcl, rank, turn++, lost, sh);
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          if (DONE && (resets >> k & 1u)) st[i] = 0.0f;
+          st[i] = __fmaf_rn(bt[k][i], __fsub_rn(xt[k][i], st[i]), st[i]);
+        }
+        if (mine && t0 + k < A.len) store_vec(h + (t0 + k) * A.h.st, st);
+      }
+    }
+    if (A.h_last && mine && rank == 0 && group == 0) {
+      const bool end = DONE && done_at(A, b, A.len - 1);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) A.h_last[b * A.channels + c + i] = end ? 0.0f : carry[i];
+    }
+  }
+  if (CLT > 1) cluster_sync();  // none leaves while another one may post to it
+}
+
+// Backward: the same on the steps in reverse order, step o of the walk being t = len - 1 - o, with
+// mu -> a (dh + mu) as a step's map.  part [batch * CLT][channels]: sums of dgate (or null).
+template <class T, int VEC, bool DONE, int CLT>
+__global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl, int64_t tiles, float* part) {
+  constexpr int S = kTileSteps;
+  extern __shared__ uint4 slots[];
+  __shared__ TileShared<CLT> sh;
+  const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32;
+  const int LC = 1 << lcl, cl = lane & (LC - 1), group = warp * (32 >> lcl) + (lane >> lcl);
+  const int TB = (int)(blockDim.x >> lcl) * S;
+  const uint32_t rank = CLT == 1 ? 0u : cluster_rank();
+  pdl_trigger();
+  if (CLT > 1) {
+    if (threadIdx.x < 2) tcx::mbar_init(&sh.bar[threadIdx.x], 1);
+    tcx::mbar_fence_init();
+    cluster_sync();
+  }
+  const int64_t per = (A.channels + LC * VEC - 1) / (LC * VEC);
+  const int64_t rounds = (A.len + (int64_t)CLT * TB - 1) / ((int64_t)CLT * TB);
+  Ahead<T, VEC, 4, S> in;
+  in.slot = reinterpret_cast<T*>(slots);
+  uint32_t turn = 0;
+  bool lost = false;
+  for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
+    const int64_t b = tile / per, c = ((tile - b * per) * LC + cl) * VEC;
+    const bool mine = c < A.channels;
+    const T* gate = at<const T>(A.gate, b, 0, c);
+    const T* x = at<const T>(A.x, b, 0, c);
+    const T* dh = at<const T>(A.dh, b, 0, c);
+    const T* h = at<const T>(A.h, b, 0, c);
+    T* dx = at<T>(A.dx, b, 0, c);
+    T* dgate = at<T>(A.dgate, b, 0, c);
+    uint8_t next[S + 1] = {};  // of the round to come: done at the walk's steps, and at the one behind them
+    const auto bring = [&](int64_t o0) {
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        const int64_t t = A.len - 1 - (o0 + k);
+        if (t >= 0 && mine) {
+          in.bring(0, k, gate + t * A.gate.st);
+          in.bring(1, k, x + t * A.x.st);
+          in.bring(2, k, dh + t * A.dh.st);
+          if (t > 0) in.bring(3, k, h + (t - 1) * A.h.st);
+        }
+        if (DONE) next[k] = t >= 0 ? done_byte(A, b, t) : (uint8_t)0;
+      }
+      const int64_t t = A.len - 1 - (o0 + S);
+      if (DONE) next[S] = t >= 0 ? done_byte(A, b, t) : (uint8_t)0;
+      if (VEC > 1) copy_commit();
+    };
+    int64_t o0 = (int64_t)rank * TB + group * S;
+    bring(o0);
+    float bias[VEC], carry[VEC], db[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) bias[i] = carry[i] = db[i] = 0.0f;
+    if (mine) {
+      load_row<VEC>(A.bias, c, bias);
+      load_row<VEC>(A.dh_last, b * A.channels + c, carry);
+    }
+    for (int64_t round = 0; round < rounds; ++round, o0 += (int64_t)CLT * TB) {
+      float bt[S][VEC], qt[S][VEC], dt[S][VEC], a[VEC], m[VEC], mu[VEC];  // 1 - a; a (1 - a) (s - x); dh
+      if (VEC > 1) copy_wait_all();
+      uint32_t ends = 0;
+      if (DONE) {
+#pragma unroll
+        for (int k = 0; k <= S; ++k) ends |= (uint32_t)(next[k] != 0) << k;
+      }
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        const int64_t t = A.len - 1 - (o0 + k);
+        const bool live = mine && t >= 0;
+        float g[VEC], xv[VEC], s[VEC];
+        in.take(0, k, g);
+        in.take(1, k, xv);
+        in.take(2, k, dt[k]);
+        in.take(3, k, s);
+        if (live && t == 0) load_row<VEC>(A.h0, b * A.channels + c, s);
+        const bool fresh = DONE && (ends >> (k + 1) & 1u);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const Gate q = gate_of(__fadd_rn(g[i], bias[i]));
+          bt[k][i] = live ? q.b : 0.0f;
+          qt[k][i] = live ? __fmul_rn(q.ab, __fsub_rn(fresh ? 0.0f : s[i], xv[i])) : 0.0f;
+          if (!live) dt[k][i] = 0.0f;
+        }
+      }
+      if (round + 1 < rounds) bring(o0 + (int64_t)CLT * TB);
+      const uint32_t own = ends & ((1u << S) - 1u);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        a[i] = 1.0f;
+        m[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < S; ++k) {
+          const float lam = DONE && (own >> k & 1u) ? dt[k][i] : __fadd_rn(dt[k][i], m[i]);
+          m[i] = __fmaf_rn(-bt[k][i], lam, lam);
+          a[i] = __fmaf_rn(-bt[k][i], a[i], a[i]);
+        }
+        if (DONE && own) a[i] = kForget;
+      }
+      tile_states<VEC, CLT>(a, m, carry, mu, lcl, rank, turn++, lost, sh);
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        const int64_t t = A.len - 1 - (o0 + k);
+        float ox[VEC], og[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float lam = DONE && (own >> k & 1u) ? dt[k][i] : __fadd_rn(dt[k][i], mu[i]);
+          ox[i] = __fmul_rn(bt[k][i], lam);
+          og[i] = __fmul_rn(qt[k][i], lam);
+          if (mine && t >= 0) db[i] = __fadd_rn(db[i], og[i]);
+          mu[i] = __fmaf_rn(-bt[k][i], lam, lam);
+        }
+        if (mine && t >= 0) {
+          store_vec(dx + t * A.dx.st, ox);
+          store_vec(dgate + t * A.dgate.st, og);
+        }
+      }
+    }
+    if (A.dh0 && mine && rank == 0 && group == 0) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) A.dh0[b * A.channels + c + i] = carry[i];
+    }
+    if (part) {  // the block's sums of its steps, groups and warps in order
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        float v = db[i];
+        for (int d = 16 >> lcl; d > 0; d /= 2) v = __fadd_rn(v, __shfl_down_sync(0xffffffffu, v, d << lcl));
+        if (lane < LC) sh.table[0][warp][0][cl * VEC + i] = v;
+      }
+      __syncthreads();
+      for (int j = (int)threadIdx.x; j < LC * VEC; j += (int)blockDim.x) {
+        const int64_t ch = (tile - b * per) * LC * VEC + j;
+        float v = 0.0f;
+        for (int w = 0; w < (int)blockDim.x / 32; ++w) v = __fadd_rn(v, sh.table[0][w][0][j]);
+        if (ch < A.channels) part[(b * CLT + rank) * A.channels + ch] = v;
+      }
+      __syncthreads();
+    }
+  }
+  if (CLT > 1) cluster_sync();
+}
+
+// dbias[c] = the sum over the rows of part [rows][channels]: 32 channels per block, 32 rows at a time,
+// joined in a fixed order.
+__global__ void __launch_bounds__(1024) k_scan_dbias(const float* part, int64_t rows, int64_t channels, float* dbias) {
+  __shared__ float sh[32][33];
+  const int cl = threadIdx.x & 31, rl = (int)threadIdx.x / 32;
+  const int64_t c = (int64_t)blockIdx.x * 32 + cl;
+  pdl_wait();
+  float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (c < channels) {
+    int64_t r = rl;
+    for (; r + 96 < rows; r += 128)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = __fadd_rn(v[u], part[(r + 32 * u) * channels + c]);
+    for (; r < rows; r += 32) v[0] = __fadd_rn(v[0], part[r * channels + c]);
+  }
+  sh[rl][cl] = __fadd_rn(__fadd_rn(v[0], v[1]), __fadd_rn(v[2], v[3]));
+  __syncthreads();
+  const float s = sum_lanes(sh[cl][rl]);
+  if (cl == 0 && (int64_t)blockIdx.x * 32 + rl < channels) dbias[(int64_t)blockIdx.x * 32 + rl] = s;
+}
+
+// How a call is cut: lanes per row of channels (log2), warps per block, blocks per cluster.
+struct ScanPlan {
+  bool columns;
+  int lcl, warps, cluster;
+  int64_t tiles;
+};
+ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, int vec, int max_warps) {
+  ScanPlan p{};
+  p.columns = len <= kColSteps;
+  const int most = vec == 1 ? 5 : 4;  // 32 or 64 channels
+  while (p.lcl < most && ((int64_t)vec << p.lcl) < channels) ++p.lcl;
+  const int64_t per = (channels + ((int64_t)vec << p.lcl) - 1) / ((int64_t)vec << p.lcl);
+  p.tiles = batch * per;
+  const int64_t steps = (int64_t)(32 >> p.lcl) * kTileSteps;  // per warp
+  p.warps = 1;
+  while (p.warps < max_warps && p.warps * steps < len) p.warps *= 2;
+  p.cluster = 1;
+  // clusters post whole vectors of 4 channels
+  const int64_t want = (int64_t)sm_count() * 2;
+  if (vec == 4)
+    while (p.cluster < kMaxCluster && p.warps >= p.cluster * 2 && p.tiles * p.cluster < want && p.warps * steps * p.cluster < len) p.cluster *= 2;
+  return p;
 }
 
 template <class T>
-__global__ void __launch_bounds__(kColThreads) k_scan_grad_columns(simx_scan A, float* dbias_part) {
-  const int64_t col = (int64_t)blockIdx.x * kColThreads + threadIdx.x;
-  if (col >= A.batch * A.channels) return;
-  const int64_t b = col / A.channels, c = col - b * A.channels;
-  const float bias = A.bias ? A.bias[c] : 0.0f;
-  float mu = A.dh_last ? A.dh_last[col] : 0.0f;
-  float db = 0.0f;
-  for (int64_t t = A.len - 1; t >= 0; --t) {
-    const Gate g = gate_of(__fadd_rn(widen(*at<const T>(A.gate, b, t, c)), bias));
-    const bool done = A.done && A.done[b * A.done_sb + t * A.done_st];
-    float lam = widen(*at<const T>(A.dh, b, t, c));
-    if (!done) lam = __fadd_rn(lam, mu);
-    float s = 0.0f;
-    if (t == 0) s = A.h0 ? A.h0[col] : 0.0f;
-    else if (!(A.done && A.done[b * A.done_sb + (t - 1) * A.done_st])) s = widen(*at<const T>(A.h, b, t - 1, c));
-    const float dg = __fmul_rn(__fmul_rn(lam, __fsub_rn(s, widen(*at<const T>(A.x, b, t, c)))), __fmul_rn(g.a, g.b));
-    *at<T>(A.dx, b, t, c) = narrow<T>(__fmul_rn(lam, g.b));
-    *at<T>(A.dgate, b, t, c) = narrow<T>(dg);
-    db = __fadd_rn(db, dg);
-    mu = __fmaf_rn(-g.b, lam, lam);
-  }
-  if (A.dh0) A.dh0[col] = mu;
-  if (dbias_part) dbias_part[col] = db;
+bool vectors(const simx_scan& a, const simx_seq& q) {
+  const int64_t bytes = 4 * (int64_t)sizeof(T);
+  return (reinterpret_cast<uintptr_t>(q.p) % (uintptr_t)bytes) == 0 && (a.batch == 1 || q.sb % 4 == 0) && (a.len == 1 || q.st % 4 == 0);
 }
 
-// dbias[c] = sum over the rows of part [rows][channels], in order.
-__global__ void __launch_bounds__(kColThreads) k_scan_dbias(const float* part, int64_t rows, int64_t channels, float* dbias) {
-  const int64_t c = (int64_t)blockIdx.x * kColThreads + threadIdx.x;
-  if (c >= channels) return;
-  double v = 0.0;
-  for (int64_t r = 0; r < rows; ++r) v += (double)part[r * channels + c];
-  dbias[c] = (float)v;
+template <class K, class... Args>
+cudaError_t launch_tiles(K* kernel, const ScanPlan& p, size_t smem, cudaStream_t s, Args... args) {
+  cudaError_t e = allow_smem(kernel, 128 * 1024);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute at[1];
+  const int64_t teams = std::min<int64_t>(p.tiles, (int64_t)1 << 24);
+  lc.gridDim = dim3((unsigned)(teams * p.cluster));
+  lc.blockDim = dim3((unsigned)(p.warps * 32));
+  lc.dynamicSmemBytes = smem;
+  lc.stream = s;
+  if (p.cluster > 1) {
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)p.cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    lc.attrs = at;
+    lc.numAttrs = 1;
+  }
+  count_launches(1);
+  return cudaLaunchKernelEx(&lc, kernel, args...);
+}
+
+template <class T, int VEC, bool DONE>
+cudaError_t scan_tiles(const simx_scan& a, const ScanPlan& p, cudaStream_t s) {
+  const size_t smem = VEC == 1 ? 0 : (size_t)p.warps * 32 * 2 * kTileSteps * VEC * sizeof(T);
+  if (VEC > 1) {
+    if (p.cluster == 2) return launch_tiles(k_scan_tiles<T, 4, DONE, 2>, p, smem, s, a, p.lcl, p.tiles);
+    if (p.cluster == 4) return launch_tiles(k_scan_tiles<T, 4, DONE, 4>, p, smem, s, a, p.lcl, p.tiles);
+    if (p.cluster == 8) return launch_tiles(k_scan_tiles<T, 4, DONE, 8>, p, smem, s, a, p.lcl, p.tiles);
+  }
+  return launch_tiles(k_scan_tiles<T, VEC, DONE, 1>, p, smem, s, a, p.lcl, p.tiles);
+}
+template <class T, int VEC, bool DONE>
+cudaError_t scan_grad_tiles(const simx_scan& a, const ScanPlan& p, float* part, cudaStream_t s) {
+  const size_t smem = VEC == 1 ? 0 : (size_t)p.warps * 32 * 4 * kTileSteps * VEC * sizeof(T);
+  if (VEC > 1) {
+    if (p.cluster == 2) return launch_tiles(k_scan_grad_tiles<T, 4, DONE, 2>, p, smem, s, a, p.lcl, p.tiles, part);
+    if (p.cluster == 4) return launch_tiles(k_scan_grad_tiles<T, 4, DONE, 4>, p, smem, s, a, p.lcl, p.tiles, part);
+    if (p.cluster == 8) return launch_tiles(k_scan_grad_tiles<T, 4, DONE, 8>, p, smem, s, a, p.lcl, p.tiles, part);
+  }
+  return launch_tiles(k_scan_grad_tiles<T, VEC, DONE, 1>, p, smem, s, a, p.lcl, p.tiles, part);
+}
+
+constexpr int kFwdWarps = 8, kGradWarps = 4;
+
+template <class T>
+cudaError_t scan(const simx_scan& a, cudaStream_t s) {
+  const bool v4 = a.channels % 4 == 0 && (a.len == 0 || (vectors<T>(a, a.x) && vectors<T>(a, a.gate) && vectors<T>(a, a.h)));
+  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4 ? 4 : 1, kFwdWarps);
+  if (p.columns) {
+    const int64_t cols = a.batch * (v4 ? a.channels / 4 : a.channels);
+    const unsigned blocks = (unsigned)((cols + kColThreads - 1) / kColThreads);
+    if (v4) k_scan_columns<T, 4><<<blocks, kColThreads, 0, s>>>(a);
+    else k_scan_columns<T, 1><<<blocks, kColThreads, 0, s>>>(a);
+    count_launches(1);
+    return cudaGetLastError();
+  }
+  if (v4) return a.done ? scan_tiles<T, 4, true>(a, p, s) : scan_tiles<T, 4, false>(a, p, s);
+  return a.done ? scan_tiles<T, 1, true>(a, p, s) : scan_tiles<T, 1, false>(a, p, s);
+}
+
+template <class T>
+cudaError_t scan_grad(const simx_scan& a, float* part, int64_t& rows, cudaStream_t s) {
+  const bool v4 = a.channels % 4 == 0 && (a.len == 0 || (vectors<T>(a, a.x) && vectors<T>(a, a.gate) && vectors<T>(a, a.h) &&
+                                                         vectors<T>(a, a.dh) && vectors<T>(a, a.dx) && vectors<T>(a, a.dgate)));
+  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4 ? 4 : 1, kGradWarps);
+  rows = a.batch * (p.columns ? 1 : p.cluster);
+  if (p.columns) {
+    const int64_t cols = a.batch * (v4 ? a.channels / 4 : a.channels);
+    const unsigned blocks = (unsigned)((cols + kColThreads - 1) / kColThreads);
+    if (v4) k_scan_grad_columns<T, 4><<<blocks, kColThreads, 0, s>>>(a, part);
+    else k_scan_grad_columns<T, 1><<<blocks, kColThreads, 0, s>>>(a, part);
+    count_launches(1);
+    return cudaGetLastError();
+  }
+  if (v4) return a.done ? scan_grad_tiles<T, 4, true>(a, p, part, s) : scan_grad_tiles<T, 4, false>(a, p, part, s);
+  return a.done ? scan_grad_tiles<T, 1, true>(a, p, part, s) : scan_grad_tiles<T, 1, false>(a, p, part, s);
 }
 
 }  // namespace
 
-size_t scan_workspace_bytes(int64_t batch, int64_t, int64_t channels) {
-  return (size_t)batch * (size_t)channels * sizeof(float);
+// The backward pass's sums of dgate: a row of channels per batch entry and block of a cluster (the plan of
+// aligned tensors, whose clusters may be larger than one).
+size_t scan_workspace_bytes(int64_t batch, int64_t len, int64_t channels) {
+  const ScanPlan p = plan_scan(batch, len, channels, 4, kGradWarps);
+  return (size_t)batch * (size_t)(p.columns ? 1 : p.cluster) * (size_t)channels * sizeof(float);
 }
 
 cudaError_t launch_scan(const simx_scan& a, cudaStream_t s) {
-  const int64_t blocks = (a.batch * a.channels + kColThreads - 1) / kColThreads;
-  if (a.dtype == SIMX_F32) k_scan_columns<float><<<(unsigned)blocks, kColThreads, 0, s>>>(a);
-  else k_scan_columns<__nv_bfloat16><<<(unsigned)blocks, kColThreads, 0, s>>>(a);
-  count_launches(1);
-  return cudaGetLastError();
+  return a.dtype == SIMX_F32 ? scan<float>(a, s) : scan<__nv_bfloat16>(a, s);
 }
 
 cudaError_t launch_scan_grad(const simx_scan& a, void* ws, cudaStream_t s) {
-  const int64_t blocks = (a.batch * a.channels + kColThreads - 1) / kColThreads;
   float* part = a.dbias ? static_cast<float*>(ws) : nullptr;
-  if (a.dtype == SIMX_F32) k_scan_grad_columns<float><<<(unsigned)blocks, kColThreads, 0, s>>>(a, part);
-  else k_scan_grad_columns<__nv_bfloat16><<<(unsigned)blocks, kColThreads, 0, s>>>(a, part);
+  int64_t rows = 0;
+  cudaError_t e = a.dtype == SIMX_F32 ? scan_grad<float>(a, part, rows, s) : scan_grad<__nv_bfloat16>(a, part, rows, s);
+  if (e != cudaSuccess || !part) return e;
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.gridDim = dim3((unsigned)((a.channels + 31) / 32));
+  lc.blockDim = dim3(1024);
+  lc.stream = s;
+  lc.attrs = at;
+  lc.numAttrs = 1;
   count_launches(1);
-  if (part) {
-    k_scan_dbias<<<(unsigned)((a.channels + kColThreads - 1) / kColThreads), kColThreads, 0, s>>>(part, a.batch, a.channels, a.dbias);
-    count_launches(1);
-  }
-  return cudaGetLastError();
+  e = cudaLaunchKernelEx(&lc, k_scan_dbias, (const float*)part, rows, a.channels, a.dbias);
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace simx
