@@ -27,18 +27,19 @@ using namespace seq;
 
 namespace {
 
-// b = sigmoid(-z) and ab = sigmoid(z) sigmoid(-z), each to relative precision.
+// b = sigmoid(-z) = 1 / (1 + 2^t) with t = z log2 e, to relative precision whatever the sign of z (2^t may
+// be inf: b is 0 then); t is one fma of the gate and the bias times log2 e.
+__device__ __forceinline__ float sigmoid_neg(float t) { return rcp(__fadd_rn(1.0f, ex2(t))); }
+// The same with ab = sigmoid(z) sigmoid(-z) = 2^t b b, t held below 2^126 (its minimum keeps a NaN).
 struct Gate {
   float b, ab;
 };
-__device__ __forceinline__ Gate gate_of(float z) {
-  const float e = ex2(__fmul_rn(-fabsf(z), kLog2e));
-  const float r = rcp(__fadd_rn(1.0f, e));
-  const float er = __fmul_rn(e, r);
+__device__ __forceinline__ Gate gate_of(float t) {
+  asm("min.NaN.f32 %0, %0, 0f42FC0000;" : "+f"(t));
+  const float e = ex2(t);
   Gate g;
-  g.b = z >= 0.0f ? er : r;
-  g.ab = __fmul_rn(er, r);
-  if (z != z) g.b = g.ab = z;
+  g.b = rcp(__fadd_rn(1.0f, e));
+  g.ab = __fmul_rn(__fmul_rn(e, g.b), g.b);
   return g;
 }
 
@@ -87,6 +88,13 @@ __device__ __forceinline__ void load_row(const float* p, int64_t off, float (&v)
   for (int i = 0; i < VEC; ++i) v[i] = p ? p[off + i] : 0.0f;
 }
 
+// bias log2 e
+template <int VEC>
+__device__ __forceinline__ void load_bias(const float* p, int64_t off, float (&v)[VEC]) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) v[i] = p ? __fmul_rn(p[off + i], kLog2e) : 0.0f;
+}
+
 // ---------------------------------------------------------------------------
 // Short sequences: a thread per column (VEC channels), through time.  The single-token step.
 // ---------------------------------------------------------------------------
@@ -108,14 +116,14 @@ __global__ void __launch_bounds__(kColThreads) k_scan_columns(simx_scan A) {
     load_vec(at<const T>(A.x, b, t, c), x[t]);
     end[t] = A.done && done_at(A, b, t);
   }
-  load_row<VEC>(A.bias, c, bias);
+  load_bias<VEC>(A.bias, c, bias);
   load_row<VEC>(A.h0, b * A.channels + c, s);
 #pragma unroll
   for (int t = 0; t < kColSteps; ++t) {
     if (t >= A.len) break;
 #pragma unroll
     for (int i = 0; i < VEC; ++i)
-      s[i] = __fmaf_rn(gate_of(__fadd_rn(g[t][i], bias[i])).b, __fsub_rn(x[t][i], s[i]), s[i]);
+      s[i] = __fmaf_rn(sigmoid_neg(__fmaf_rn(g[t][i], kLog2e, bias[i])), __fsub_rn(x[t][i], s[i]), s[i]);
     store_vec(at<T>(A.h, b, t, c), s);
     if (end[t]) {
 #pragma unroll
@@ -136,7 +144,7 @@ __global__ void __launch_bounds__(kColThreads) k_scan_grad_columns(simx_scan A, 
   if (col >= cols) return;
   const int64_t b = col / per, c = (col - b * per) * VEC;
   float bias[VEC], mu[VEC], db[VEC];
-  load_row<VEC>(A.bias, c, bias);
+  load_bias<VEC>(A.bias, c, bias);
   load_row<VEC>(A.dh_last, b * A.channels + c, mu);
 #pragma unroll
   for (int i = 0; i < VEC; ++i) db[i] = 0.0f;
@@ -150,7 +158,7 @@ __global__ void __launch_bounds__(kColThreads) k_scan_grad_columns(simx_scan A, 
     const bool fresh = t > 0 && A.done && done_at(A, b, t - 1), end = A.done && done_at(A, b, t);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-      const Gate q = gate_of(__fadd_rn(g[i], bias[i]));
+      const Gate q = gate_of(__fmaf_rn(g[i], kLog2e, bias[i]));
       const float lam = end ? dh[i] : __fadd_rn(dh[i], mu[i]);
       dx[i] = __fmul_rn(q.b, lam);
       dg[i] = __fmul_rn(__fmul_rn(q.ab, __fsub_rn(fresh ? 0.0f : s[i], x[i])), lam);
@@ -181,57 +189,82 @@ constexpr float kForget = -1.0f;
 constexpr int kMaxWarps = 8;
 constexpr int kMaxCluster = 8;
 
+// FORGET: whether maps may be marked so.
+template <bool FORGET>
 __device__ __forceinline__ float apply(float A, float B, float s) {
-  return A < 0.0f ? B : __fmaf_rn(A, s, B);
+  return FORGET && A < 0.0f ? B : __fmaf_rn(A, s, B);
 }
 // (A, B) after (pA, pB)
+template <bool FORGET>
 __device__ __forceinline__ void compose(float pA, float pB, float& A, float& B) {
-  B = apply(A, B, pB);
-  A = A < 0.0f || pA < 0.0f ? kForget : __fmul_rn(pA, A);
+  B = apply<FORGET>(A, B, pB);
+  A = FORGET && (A < 0.0f || pA < 0.0f) ? kForget : __fmul_rn(pA, A);
 }
 
 template <int CLT>
 struct TileShared {
-  float4 peer[2][CLT][2][16];  // [parity][rank][A or B]: 64 channels
+  float4 peer[2][CLT][2][16];            // [parity][rank][A or B]: 64 channels
+  float4 table[2][kMaxWarps][2][16];     // [parity][warp][A or B]
   uint64_t bar[2];
-  float table[2][kMaxWarps][2][64];
 };
+
+template <int VEC>
+__device__ __forceinline__ void put4(float4* row, int cl, const float (&v)[VEC]) {
+  if (VEC == 4) row[cl] = make_float4(v[0], v[1 % VEC], v[2 % VEC], v[3 % VEC]);
+  else reinterpret_cast<float*>(row)[cl] = v[0];
+}
+template <int VEC>
+__device__ __forceinline__ void get4(const float4* row, int cl, float (&v)[VEC]) {
+  if (VEC == 4) {
+    const float4 q = row[cl];
+    const float w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = w[i];
+  } else {
+    v[0] = reinterpret_cast<const float*>(row)[cl];
+  }
+}
 
 // The state that comes into each thread's steps: on entry A, B are its map and carry the state before the
 // round, on return s is the state before its first step and carry that after the round.
-template <int VEC, int CLT>
+template <int VEC, int CLT, bool FORGET>
 __device__ __forceinline__ void tile_states(const float (&A)[VEC], const float (&B)[VEC], float (&carry)[VEC], float (&s)[VEC],
                                             int lcl, uint32_t rank, uint32_t turn, bool& lost, TileShared<CLT>& sh) {
   const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32, warps = (int)blockDim.x / 32;
   const int LC = 1 << lcl, cl = lane & (LC - 1), tg = lane >> lcl, GW = 32 >> lcl, parity = (int)(turn & 1u);
-  float pa[VEC], pb[VEC];  // the maps of the warp's groups before this one
+  float ia[VEC], ib[VEC], pa[VEC], pb[VEC];  // the maps of the warp's groups up to this one, and before it
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
     float a = A[i], b = B[i];
     for (int d = 1; d < GW; d *= 2) {
       const float qa = __shfl_up_sync(0xffffffffu, a, d << lcl), qb = __shfl_up_sync(0xffffffffu, b, d << lcl);
-      if (tg >= d) compose(qa, qb, a, b);
+      if (tg >= d) compose<FORGET>(qa, qb, a, b);
     }
-    if (tg == GW - 1) {
-      sh.table[parity][warp][0][cl * VEC + i] = a;
-      sh.table[parity][warp][1][cl * VEC + i] = b;
-    }
-    pa[i] = __shfl_up_sync(0xffffffffu, a, LC & 31);
-    pb[i] = __shfl_up_sync(0xffffffffu, b, LC & 31);
-    if (tg == 0) {
-      pa[i] = 1.0f;
-      pb[i] = 0.0f;
-    }
+    ia[i] = a;
+    ib[i] = b;
+  }
+  if (tg == GW - 1) {
+    put4(sh.table[parity][warp][0], cl, ia);
+    put4(sh.table[parity][warp][1], cl, ib);
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    pa[i] = __shfl_up_sync(0xffffffffu, ia[i], LC & 31);
+    pb[i] = __shfl_up_sync(0xffffffffu, ib[i], LC & 31);
   }
   __syncthreads();
   if (CLT == 1) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) s[i] = carry[i];
+#pragma unroll 4
     for (int w = 0; w < warps; ++w) {
+      float a[VEC], b[VEC];
+      get4(sh.table[parity][w][0], cl, a);
+      get4(sh.table[parity][w][1], cl, b);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         if (w == warp) s[i] = carry[i];
-        carry[i] = apply(sh.table[parity][w][0][cl * VEC + i], sh.table[parity][w][1][cl * VEC + i], carry[i]);
+        carry[i] = apply<FORGET>(a[i], b[i], carry[i]);
       }
     }
   } else {
@@ -241,17 +274,20 @@ __device__ __forceinline__ void tile_states(const float (&A)[VEC], const float (
       ta[i] = wa[i] = 1.0f;
       tb[i] = wb[i] = 0.0f;
     }
+#pragma unroll 4
     for (int w = 0; w < warps; ++w) {
+      float a[VEC], b[VEC];
+      get4(sh.table[parity][w][0], cl, a);
+      get4(sh.table[parity][w][1], cl, b);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         if (w == warp) {
           wa[i] = ta[i];
           wb[i] = tb[i];
         }
-        float a = sh.table[parity][w][0][cl * VEC + i], b = sh.table[parity][w][1][cl * VEC + i];
-        compose(ta[i], tb[i], a, b);
-        ta[i] = a;
-        tb[i] = b;
+        compose<FORGET>(ta[i], tb[i], a[i], b[i]);
+        ta[i] = a[i];
+        tb[i] = b[i];
       }
     }
     // Warp w posts to block w of the cluster.  A block may post a round while another still reads the one
@@ -266,12 +302,13 @@ __device__ __forceinline__ void tile_states(const float (&A)[VEC], const float (
     lost = lost || !tcx::mbar_wait(bar, (turn >> 1) & 1u, kPeerCycles);
 #pragma unroll
     for (int r = 0; r < CLT; ++r) {
-      const float4 a = sh.peer[parity][r][0][cl], b = sh.peer[parity][r][1][cl];
-      const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+      float a[VEC], b[VEC];
+      get4(sh.peer[parity][r][0], cl, a);
+      get4(sh.peer[parity][r][1], cl, b);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        if (r == (int)rank) s[i] = apply(wa[i], wb[i], carry[i]);
-        carry[i] = apply(av[i], bv[i], carry[i]);
+        if (r == (int)rank) s[i] = apply<FORGET>(wa[i], wb[i], carry[i]);
+        carry[i] = apply<FORGET>(a[i], b[i], carry[i]);
       }
     }
     if (lost) {  // a post that never came: what the cluster still computes is NaN
@@ -279,8 +316,10 @@ __device__ __forceinline__ void tile_states(const float (&A)[VEC], const float (
       for (int i = 0; i < VEC; ++i) s[i] = carry[i] = nan();
     }
   }
+  if (tg > 0) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) s[i] = apply(pa[i], pb[i], s[i]);
+    for (int i = 0; i < VEC; ++i) s[i] = apply<FORGET>(pa[i], pb[i], s[i]);
+  }
 }
 
 // Elements of K tensors on their way: VEC = 4 in the thread's places in shared memory, VEC = 1 in
@@ -288,14 +327,24 @@ __device__ __forceinline__ void tile_states(const float (&A)[VEC], const float (
 template <class T, int VEC, int K, int S>
 struct Ahead {
   T reg[VEC == 1 ? K * S : 1];
-  T* slot;  // [K * S][threads][VEC]
+  T* slot;  // the thread's places, `pitch` elements apart
+  int pitch;
+  __device__ __forceinline__ void start(void* shared) {
+    slot = static_cast<T*>(shared) + (int)threadIdx.x * VEC;
+    pitch = (int)blockDim.x * VEC;
+  }
   __device__ __forceinline__ void bring(int k, int s, const T* p) {
     if (VEC == 1) reg[(k * S + s) % (VEC == 1 ? K * S : 1)] = *p;
-    else copy_async<VEC * (int)sizeof(T) < 4 ? 4 : VEC * (int)sizeof(T)>(slot + ((int64_t)(k * S + s) * blockDim.x + threadIdx.x) * VEC, p);
+    else copy_async<VEC * (int)sizeof(T) < 4 ? 4 : VEC * (int)sizeof(T)>(slot + (k * S + s) * pitch, p);
+  }
+  // Steps 0 .. S - 1 at p, p + st, ...
+  __device__ __forceinline__ void bring_all(int k, const T* p, int64_t st) {
+#pragma unroll
+    for (int s = 0; s < S; ++s, p += st) bring(k, s, p);
   }
   __device__ __forceinline__ void take(int k, int s, float (&v)[VEC]) const {
     if (VEC == 1) v[0] = widen(reg[(k * S + s) % (VEC == 1 ? K * S : 1)]);
-    else load_vec(slot + ((int64_t)(k * S + s) * blockDim.x + threadIdx.x) * VEC, v);
+    else load_vec(slot + (k * S + s) * pitch, v);
   }
 };
 
@@ -318,39 +367,50 @@ __global__ void __launch_bounds__(256, 2) k_scan_tiles(simx_scan A, int lcl, int
   const int64_t per = (A.channels + LC * VEC - 1) / (LC * VEC);
   const int64_t rounds = (A.len + (int64_t)CLT * TB - 1) / ((int64_t)CLT * TB);
   Ahead<T, VEC, 2, S> in;
-  in.slot = reinterpret_cast<T*>(slots);
+  in.start(slots);
   uint32_t turn = 0;
   bool lost = false;
   for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
     const int64_t b = tile / per, c = ((tile - b * per) * LC + cl) * VEC;
     const bool mine = c < A.channels;
-    const T* gate = at<const T>(A.gate, b, 0, c);
-    const T* x = at<const T>(A.x, b, 0, c);
-    T* h = at<T>(A.h, b, 0, c);
+    int64_t t0 = (int64_t)rank * TB + group * S;
+    const T* gate = at<const T>(A.gate, b, t0, c);  // of the round to come
+    const T* x = at<const T>(A.x, b, t0, c);
+    T* h = at<T>(A.h, b, t0, c);                    // of the round at hand
+    const int64_t step = (int64_t)CLT * TB;
     uint8_t next[S] = {};  // of the round to come: whether the state before a step is dropped
-    const auto bring = [&](int64_t t0) {
+    const auto bring = [&](int64_t u) {
+      if (mine && u + S <= A.len) {
+        in.bring_all(0, gate, A.gate.st);
+        in.bring_all(1, x, A.x.st);
+      } else if (mine) {
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-        const int64_t t = t0 + s;
-        if (t < A.len && mine) {
-          in.bring(0, s, gate + t * A.gate.st);
-          in.bring(1, s, x + t * A.x.st);
+        for (int k = 0; k < S; ++k) {
+          if (u + k < A.len) {
+            in.bring(0, k, gate + k * A.gate.st);
+            in.bring(1, k, x + k * A.x.st);
+          }
         }
-        if (DONE) next[s] = t > 0 && t < A.len ? done_byte(A, b, t - 1) : (uint8_t)0;
       }
       if (VEC > 1) copy_commit();
+      gate += step * A.gate.st;
+      x += step * A.x.st;
+      if (DONE) {
+#pragma unroll
+        for (int k = 0; k < S; ++k) next[k] = u + k > 0 && u + k < A.len ? done_byte(A, b, u + k - 1) : (uint8_t)0;
+      }
     };
-    int64_t t0 = (int64_t)rank * TB + group * S;
     bring(t0);
     float bias[VEC], carry[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) bias[i] = carry[i] = 0.0f;
     if (mine) {
-      load_row<VEC>(A.bias, c, bias);
+      load_bias<VEC>(A.bias, c, bias);
       load_row<VEC>(A.h0, b * A.channels + c, carry);
     }
-    for (int64_t round = 0; round < rounds; ++round, t0 += (int64_t)CLT * TB) {
+    for (int64_t round = 0; round < rounds; ++round, t0 += step, h += step * A.h.st) {
       float bt[S][VEC], xt[S][VEC], a[VEC], s[VEC], st[VEC];
+      const bool whole = mine && t0 + S <= A.len;
       if (VEC > 1) copy_wait_all();
       uint32_t resets = 0;
       if (DONE) {
@@ -359,17 +419,20 @@ __global__ void __launch_bounds__(256, 2) k_scan_tiles(simx_scan A, int lcl, int
       }
 #pragma unroll
       for (int k = 0; k < S; ++k) {
-        const bool live = mine && t0 + k < A.len;
         float g[VEC];
         in.take(0, k, g);
         in.take(1, k, xt[k]);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          bt[k][i] = live ? gate_of(__fadd_rn(g[i], bias[i])).b : 0.0f;  // past the end: the state stays
-          if (!live) xt[k][i] = 0.0f;
-        }
+        for (int i = 0; i < VEC; ++i) bt[k][i] = sigmoid_neg(__fmaf_rn(g[i], kLog2e, bias[i]));
       }
-      if (round + 1 < rounds) bring(t0 + (int64_t)CLT * TB);
+      if (!whole) {  // steps past the end leave the state as it is
+#pragma unroll
+        for (int k = 0; k < S; ++k)
+          if (!mine || t0 + k >= A.len)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) bt[k][i] = xt[k][i] = 0.0f;
+      }
+      if (round + 1 < rounds) bring(t0 + step);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         a[i] = 1.0f;
@@ -382,15 +445,16 @@ __global__ void __launch_bounds__(256, 2) k_scan_tiles(simx_scan A, int lcl, int
         }
         if (DONE && resets) a[i] = kForget;
       }
-      tile_states<VEC, CLT>(a, s, carry, st, lcl, rank, turn++, lost, sh);
+      tile_states<VEC, CLT, DONE>(a, s, carry, st, lcl, rank, turn++, lost, sh);
+      T* p = h;
 #pragma unroll
-      for (int k = 0; k < S; ++k) {
+      for (int k = 0; k < S; ++k, p += A.h.st) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
           if (DONE && (resets >> k & 1u)) st[i] = 0.0f;
           st[i] = __fmaf_rn(bt[k][i], __fsub_rn(xt[k][i], st[i]), st[i]);
         }
-        if (mine && t0 + k < A.len) store_vec(h + (t0 + k) * A.h.st, st);
+        if (whole || (mine && t0 + k < A.len)) store_vec(p, st);
       }
     }
     if (A.h_last && mine && rank == 0 && group == 0) {
@@ -422,46 +486,59 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
   const int64_t per = (A.channels + LC * VEC - 1) / (LC * VEC);
   const int64_t rounds = (A.len + (int64_t)CLT * TB - 1) / ((int64_t)CLT * TB);
   Ahead<T, VEC, 4, S> in;
-  in.slot = reinterpret_cast<T*>(slots);
+  in.start(slots);
   uint32_t turn = 0;
   bool lost = false;
   for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
     const int64_t b = tile / per, c = ((tile - b * per) * LC + cl) * VEC;
     const bool mine = c < A.channels;
-    const T* gate = at<const T>(A.gate, b, 0, c);
-    const T* x = at<const T>(A.x, b, 0, c);
-    const T* dh = at<const T>(A.dh, b, 0, c);
-    const T* h = at<const T>(A.h, b, 0, c);
-    T* dx = at<T>(A.dx, b, 0, c);
-    T* dgate = at<T>(A.dgate, b, 0, c);
+    const int64_t step = (int64_t)CLT * TB;
+    int64_t t0 = A.len - 1 - (int64_t)rank * TB - group * S;  // of the thread's first step of the walk
+    const T* gate = at<const T>(A.gate, b, t0, c);            // of the round to come
+    const T* x = at<const T>(A.x, b, t0, c);
+    const T* dh = at<const T>(A.dh, b, t0, c);
+    const T* h = at<const T>(A.h, b, t0 - 1, c);
+    T* dx = at<T>(A.dx, b, t0, c);                            // of the round at hand
+    T* dgate = at<T>(A.dgate, b, t0, c);
     uint8_t next[S + 1] = {};  // of the round to come: done at the walk's steps, and at the one behind them
-    const auto bring = [&](int64_t o0) {
+    const auto bring = [&](int64_t u) {
+      if (mine && u >= S) {
+        in.bring_all(0, gate, -A.gate.st);
+        in.bring_all(1, x, -A.x.st);
+        in.bring_all(2, dh, -A.dh.st);
+        in.bring_all(3, h, -A.h.st);
+      } else if (mine) {
 #pragma unroll
-      for (int k = 0; k < S; ++k) {
-        const int64_t t = A.len - 1 - (o0 + k);
-        if (t >= 0 && mine) {
-          in.bring(0, k, gate + t * A.gate.st);
-          in.bring(1, k, x + t * A.x.st);
-          in.bring(2, k, dh + t * A.dh.st);
-          if (t > 0) in.bring(3, k, h + (t - 1) * A.h.st);
+        for (int k = 0; k < S; ++k) {
+          if (u - k >= 0) {
+            in.bring(0, k, gate - k * A.gate.st);
+            in.bring(1, k, x - k * A.x.st);
+            in.bring(2, k, dh - k * A.dh.st);
+            if (u - k > 0) in.bring(3, k, h - k * A.h.st);
+          }
         }
-        if (DONE) next[k] = t >= 0 ? done_byte(A, b, t) : (uint8_t)0;
       }
-      const int64_t t = A.len - 1 - (o0 + S);
-      if (DONE) next[S] = t >= 0 ? done_byte(A, b, t) : (uint8_t)0;
       if (VEC > 1) copy_commit();
+      gate -= step * A.gate.st;
+      x -= step * A.x.st;
+      dh -= step * A.dh.st;
+      h -= step * A.h.st;
+      if (DONE) {
+#pragma unroll
+        for (int k = 0; k <= S; ++k) next[k] = u - k >= 0 ? done_byte(A, b, u - k) : (uint8_t)0;
+      }
     };
-    int64_t o0 = (int64_t)rank * TB + group * S;
-    bring(o0);
+    bring(t0);
     float bias[VEC], carry[VEC], db[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) bias[i] = carry[i] = db[i] = 0.0f;
     if (mine) {
-      load_row<VEC>(A.bias, c, bias);
+      load_bias<VEC>(A.bias, c, bias);
       load_row<VEC>(A.dh_last, b * A.channels + c, carry);
     }
-    for (int64_t round = 0; round < rounds; ++round, o0 += (int64_t)CLT * TB) {
+    for (int64_t round = 0; round < rounds; ++round, t0 -= step, dx -= step * A.dx.st, dgate -= step * A.dgate.st) {
       float bt[S][VEC], qt[S][VEC], dt[S][VEC], a[VEC], m[VEC], mu[VEC];  // 1 - a; a (1 - a) (s - x); dh
+      const bool whole = mine && t0 >= S;
       if (VEC > 1) copy_wait_all();
       uint32_t ends = 0;
       if (DONE) {
@@ -470,24 +547,28 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
       }
 #pragma unroll
       for (int k = 0; k < S; ++k) {
-        const int64_t t = A.len - 1 - (o0 + k);
-        const bool live = mine && t >= 0;
         float g[VEC], xv[VEC], s[VEC];
         in.take(0, k, g);
         in.take(1, k, xv);
         in.take(2, k, dt[k]);
         in.take(3, k, s);
-        if (live && t == 0) load_row<VEC>(A.h0, b * A.channels + c, s);
+        if (mine && t0 == k) load_row<VEC>(A.h0, b * A.channels + c, s);
         const bool fresh = DONE && (ends >> (k + 1) & 1u);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          const Gate q = gate_of(__fadd_rn(g[i], bias[i]));
-          bt[k][i] = live ? q.b : 0.0f;
-          qt[k][i] = live ? __fmul_rn(q.ab, __fsub_rn(fresh ? 0.0f : s[i], xv[i])) : 0.0f;
-          if (!live) dt[k][i] = 0.0f;
+          const Gate q = gate_of(__fmaf_rn(g[i], kLog2e, bias[i]));
+          bt[k][i] = q.b;
+          qt[k][i] = __fmul_rn(q.ab, __fsub_rn(fresh ? 0.0f : s[i], xv[i]));
         }
       }
-      if (round + 1 < rounds) bring(o0 + (int64_t)CLT * TB);
+      if (!whole) {  // steps before the first leave what comes to them as it is
+#pragma unroll
+        for (int k = 0; k < S; ++k)
+          if (!mine || t0 < k)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) bt[k][i] = qt[k][i] = dt[k][i] = 0.0f;
+      }
+      if (round + 1 < rounds) bring(t0 - step);
       const uint32_t own = ends & ((1u << S) - 1u);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
@@ -501,22 +582,23 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
         }
         if (DONE && own) a[i] = kForget;
       }
-      tile_states<VEC, CLT>(a, m, carry, mu, lcl, rank, turn++, lost, sh);
+      tile_states<VEC, CLT, DONE>(a, m, carry, mu, lcl, rank, turn++, lost, sh);
+      T* px = dx;
+      T* pg = dgate;
 #pragma unroll
-      for (int k = 0; k < S; ++k) {
-        const int64_t t = A.len - 1 - (o0 + k);
+      for (int k = 0; k < S; ++k, px -= A.dx.st, pg -= A.dgate.st) {
         float ox[VEC], og[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
           const float lam = DONE && (own >> k & 1u) ? dt[k][i] : __fadd_rn(dt[k][i], mu[i]);
           ox[i] = __fmul_rn(bt[k][i], lam);
           og[i] = __fmul_rn(qt[k][i], lam);
-          if (mine && t >= 0) db[i] = __fadd_rn(db[i], og[i]);
+          db[i] = __fadd_rn(db[i], og[i]);  // steps that are not there: qt is 0
           mu[i] = __fmaf_rn(-bt[k][i], lam, lam);
         }
-        if (mine && t >= 0) {
-          store_vec(dx + t * A.dx.st, ox);
-          store_vec(dgate + t * A.dgate.st, og);
+        if (whole || (mine && t0 >= k)) {
+          store_vec(px, ox);
+          store_vec(pg, og);
         }
       }
     }
@@ -530,13 +612,13 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
       for (int i = 0; i < VEC; ++i) {
         float v = db[i];
         for (int d = 16 >> lcl; d > 0; d /= 2) v = __fadd_rn(v, __shfl_down_sync(0xffffffffu, v, d << lcl));
-        if (lane < LC) sh.table[0][warp][0][cl * VEC + i] = v;
+        if (lane < LC) reinterpret_cast<float*>(sh.table[0][warp][0])[cl * VEC + i] = v;
       }
       __syncthreads();
       for (int j = (int)threadIdx.x; j < LC * VEC; j += (int)blockDim.x) {
         const int64_t ch = (tile - b * per) * LC * VEC + j;
         float v = 0.0f;
-        for (int w = 0; w < (int)blockDim.x / 32; ++w) v = __fadd_rn(v, sh.table[0][w][0][j]);
+        for (int w = 0; w < (int)blockDim.x / 32; ++w) v = __fadd_rn(v, reinterpret_cast<const float*>(sh.table[0][w][0])[j]);
         if (ch < A.channels) part[(b * CLT + rank) * A.channels + ch] = v;
       }
       __syncthreads();
