@@ -66,7 +66,7 @@ __device__ __forceinline__ float sum_lanes(float v) {
   return v;
 }
 
-// Clusters: this block's rank, a barrier of all their threads, and a store of 16 bytes into block `rank`'s
+// Clusters: this block's rank, a barrier of all their threads, and a store of 8 bytes into block `rank`'s
 // shared memory that counts them on a barrier of that block: the data carries its own signal, where a
 // cluster barrier's release would wait for every global store on its way.
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -78,12 +78,12 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void post_peer(float4* slot, uint64_t* bar, uint32_t rank, float4 v) {
+__device__ __forceinline__ void post_peer(float2* slot, uint64_t* bar, uint32_t rank, float2 v) {
   uint32_t at, on;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tcx::su32(slot)), "r"(rank));
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(on) : "r"(tcx::su32(bar)), "r"(rank));
-  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(at),
-               "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(on)
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(at), "f"(v.x),
+               "f"(v.y), "r"(on)
                : "memory");
 }
 constexpr long long kPeerCycles = 2000000000ll;  // a peer's posts take microseconds: a second is a failure

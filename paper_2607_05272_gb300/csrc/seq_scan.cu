@@ -179,15 +179,12 @@ __global__ void __launch_bounds__(kColThreads) k_scan_grad_columns(simx_scan A, 
 // Tiles of steps and channels.
 // A thread holds S consecutive steps of VEC channels; LC lanes of a warp take neighbouring channels, its
 // 32 / LC groups of lanes and the block's warps consecutive steps.  Per round a block takes
-// warps * (32 / LC) * S steps, the cluster that many of each of its blocks, in rank order, and then all
-// move on.  A thread's steps are the map s -> A s + B; the maps before it are joined by shuffles within
-// the warp, over a table of the warps' maps, and over a table of the blocks' maps that every block posts
-// to all others.  A = kForget marks a map that does not read s (an episode ended in it): what s holds,
-// infinities included, is then gone.
+// warps * (32 / LC) * S steps.  A thread's steps are the map s -> A s + B; the maps before it are joined by
+// shuffles within the warp and over a table of the warps' maps.  A = kForget marks a map that does not read
+// s (an episode ended in it): what s holds, infinities included, is then gone.
 // ---------------------------------------------------------------------------
 constexpr float kForget = -1.0f;
 constexpr int kMaxWarps = 8;
-constexpr int kMaxCluster = 8;
 
 // FORGET: whether maps may be marked so.
 template <bool FORGET>
@@ -201,11 +198,8 @@ __device__ __forceinline__ void compose(float pA, float pB, float& A, float& B) 
   A = FORGET && (A < 0.0f || pA < 0.0f) ? kForget : __fmul_rn(pA, A);
 }
 
-template <int CLT>
 struct TileShared {
-  float4 peer[2][CLT][2][16];            // [parity][rank][A or B]: 64 channels
-  float4 table[2][kMaxWarps][2][16];     // [parity][warp][A or B]
-  uint64_t bar[2];
+  float4 table[2][kMaxWarps][2][16];  // [parity][warp][A or B]: 64 channels
 };
 
 template <int VEC>
@@ -227,9 +221,9 @@ __device__ __forceinline__ void get4(const float4* row, int cl, float (&v)[VEC])
 
 // The state that comes into each thread's steps: on entry A, B are its map and carry the state before the
 // round, on return s is the state before its first step and carry that after the round.
-template <int VEC, int CLT, bool FORGET>
+template <int VEC, bool FORGET>
 __device__ __forceinline__ void tile_states(const float (&A)[VEC], const float (&B)[VEC], float (&carry)[VEC], float (&s)[VEC],
-                                            int lcl, uint32_t rank, uint32_t turn, bool& lost, TileShared<CLT>& sh) {
+                                            int lcl, uint32_t turn, TileShared& sh) {
   const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32, warps = (int)blockDim.x / 32;
   const int LC = 1 << lcl, cl = lane & (LC - 1), tg = lane >> lcl, GW = 32 >> lcl, parity = (int)(turn & 1u);
   float ia[VEC], ib[VEC], pa[VEC], pb[VEC];  // the maps of the warp's groups up to this one, and before it
@@ -253,67 +247,17 @@ __device__ __forceinline__ void tile_states(const float (&A)[VEC], const float (
     pb[i] = __shfl_up_sync(0xffffffffu, ib[i], LC & 31);
   }
   __syncthreads();
-  if (CLT == 1) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) s[i] = carry[i];
+  for (int i = 0; i < VEC; ++i) s[i] = carry[i];
 #pragma unroll 4
-    for (int w = 0; w < warps; ++w) {
-      float a[VEC], b[VEC];
-      get4(sh.table[parity][w][0], cl, a);
-      get4(sh.table[parity][w][1], cl, b);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        if (w == warp) s[i] = carry[i];
-        carry[i] = apply<FORGET>(a[i], b[i], carry[i]);
-      }
-    }
-  } else {
-    float ta[VEC], tb[VEC], wa[VEC], wb[VEC];  // the block's map, and that of the warps before this one
+  for (int w = 0; w < warps; ++w) {
+    float a[VEC], b[VEC];
+    get4(sh.table[parity][w][0], cl, a);
+    get4(sh.table[parity][w][1], cl, b);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-      ta[i] = wa[i] = 1.0f;
-      tb[i] = wb[i] = 0.0f;
-    }
-#pragma unroll 4
-    for (int w = 0; w < warps; ++w) {
-      float a[VEC], b[VEC];
-      get4(sh.table[parity][w][0], cl, a);
-      get4(sh.table[parity][w][1], cl, b);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        if (w == warp) {
-          wa[i] = ta[i];
-          wb[i] = tb[i];
-        }
-        compose<FORGET>(ta[i], tb[i], a[i], b[i]);
-        ta[i] = a[i];
-        tb[i] = b[i];
-      }
-    }
-    // Warp w posts to block w of the cluster.  A block may post a round while another still reads the one
-    // before, but not the one after: that takes the other's post of this round.
-    uint64_t* bar = &sh.bar[parity];
-    const uint32_t bytes = (uint32_t)LC * 32u;  // per block that posts, of VEC = 4
-    if (threadIdx.x == 0) tcx::mbar_arrive_expect_tx(bar, bytes * CLT);
-    if (warp < CLT && tg == 0) {
-      post_peer(&sh.peer[parity][rank][0][cl], bar, (uint32_t)warp, make_float4(ta[0], ta[1 % VEC], ta[2 % VEC], ta[3 % VEC]));
-      post_peer(&sh.peer[parity][rank][1][cl], bar, (uint32_t)warp, make_float4(tb[0], tb[1 % VEC], tb[2 % VEC], tb[3 % VEC]));
-    }
-    lost = lost || !tcx::mbar_wait(bar, (turn >> 1) & 1u, kPeerCycles);
-#pragma unroll
-    for (int r = 0; r < CLT; ++r) {
-      float a[VEC], b[VEC];
-      get4(sh.peer[parity][r][0], cl, a);
-      get4(sh.peer[parity][r][1], cl, b);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        if (r == (int)rank) s[i] = apply<FORGET>(wa[i], wb[i], carry[i]);
-        carry[i] = apply<FORGET>(a[i], b[i], carry[i]);
-      }
-    }
-    if (lost) {  // a post that never came: what the cluster still computes is NaN
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) s[i] = carry[i] = nan();
+      if (w == warp) s[i] = carry[i];
+      carry[i] = apply<FORGET>(a[i], b[i], carry[i]);
     }
   }
   if (tg > 0) {
@@ -350,34 +294,27 @@ struct Ahead {
 
 constexpr int kTileSteps = 8;
 
-template <class T, int VEC, bool DONE, int CLT>
+template <class T, int VEC, bool DONE>
 __global__ void __launch_bounds__(256, 2) k_scan_tiles(simx_scan A, int lcl, int64_t tiles) {
   constexpr int S = kTileSteps;
   extern __shared__ uint4 slots[];
-  __shared__ TileShared<CLT> sh;
+  __shared__ TileShared sh;
   const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32;
   const int LC = 1 << lcl, cl = lane & (LC - 1), group = warp * (32 >> lcl) + (lane >> lcl);
   const int TB = (int)(blockDim.x >> lcl) * S;  // steps per block and round
-  const uint32_t rank = CLT == 1 ? 0u : cluster_rank();
-  if (CLT > 1) {  // every block runs, its barriers ready, before another one posts to it
-    if (threadIdx.x < 2) tcx::mbar_init(&sh.bar[threadIdx.x], 1);
-    tcx::mbar_fence_init();
-    cluster_sync();
-  }
   const int64_t per = (A.channels + LC * VEC - 1) / (LC * VEC);
-  const int64_t rounds = (A.len + (int64_t)CLT * TB - 1) / ((int64_t)CLT * TB);
+  const int64_t rounds = (A.len + TB - 1) / TB;
   Ahead<T, VEC, 2, S> in;
   in.start(slots);
   uint32_t turn = 0;
-  bool lost = false;
-  for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int64_t b = tile / per, c = ((tile - b * per) * LC + cl) * VEC;
     const bool mine = c < A.channels;
-    int64_t t0 = (int64_t)rank * TB + group * S;
+    int64_t t0 = (int64_t)group * S;
     const T* gate = at<const T>(A.gate, b, t0, c);  // of the round to come
     const T* x = at<const T>(A.x, b, t0, c);
     T* h = at<T>(A.h, b, t0, c);                    // of the round at hand
-    const int64_t step = (int64_t)CLT * TB;
+    const int64_t step = TB;
     uint8_t next[S] = {};  // of the round to come: whether the state before a step is dropped
     const auto bring = [&](int64_t u) {
       if (mine && u + S <= A.len) {
@@ -445,7 +382,7 @@ __global__ void __launch_bounds__(256, 2) k_scan_tiles(simx_scan A, int lcl, int
         }
         if (DONE && resets) a[i] = kForget;
       }
-      tile_states<VEC, CLT, DONE>(a, s, carry, st, lcl, rank, turn++, lost, sh);
+      tile_states<VEC, DONE>(a, s, carry, st, lcl, turn++, sh);
       T* p = h;
 #pragma unroll
       for (int k = 0; k < S; ++k, p += A.h.st) {
@@ -457,43 +394,36 @@ __global__ void __launch_bounds__(256, 2) k_scan_tiles(simx_scan A, int lcl, int
         if (whole || (mine && t0 + k < A.len)) store_vec(p, st);
       }
     }
-    if (A.h_last && mine && rank == 0 && group == 0) {
+    if (A.h_last) __syncthreads();  // h_last may be h0, which every warp has used by now
+    if (A.h_last && mine && group == 0) {
       const bool end = DONE && done_at(A, b, A.len - 1);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) A.h_last[b * A.channels + c + i] = end ? 0.0f : carry[i];
     }
   }
-  if (CLT > 1) cluster_sync();  // none leaves while another one may post to it
 }
 
 // Backward: the same on the steps in reverse order, step o of the walk being t = len - 1 - o, with
-// mu -> a (dh + mu) as a step's map.  part [batch * CLT][channels]: sums of dgate (or null).
-template <class T, int VEC, bool DONE, int CLT>
+// mu -> a (dh + mu) as a step's map.  part [batch][channels]: sums of dgate (or null).
+template <class T, int VEC, bool DONE>
 __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl, int64_t tiles, float* part) {
   constexpr int S = kTileSteps;
   extern __shared__ uint4 slots[];
-  __shared__ TileShared<CLT> sh;
+  __shared__ TileShared sh;
   const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32;
   const int LC = 1 << lcl, cl = lane & (LC - 1), group = warp * (32 >> lcl) + (lane >> lcl);
   const int TB = (int)(blockDim.x >> lcl) * S;
-  const uint32_t rank = CLT == 1 ? 0u : cluster_rank();
   pdl_trigger();
-  if (CLT > 1) {
-    if (threadIdx.x < 2) tcx::mbar_init(&sh.bar[threadIdx.x], 1);
-    tcx::mbar_fence_init();
-    cluster_sync();
-  }
   const int64_t per = (A.channels + LC * VEC - 1) / (LC * VEC);
-  const int64_t rounds = (A.len + (int64_t)CLT * TB - 1) / ((int64_t)CLT * TB);
+  const int64_t rounds = (A.len + TB - 1) / TB;
   Ahead<T, VEC, 4, S> in;
   in.start(slots);
   uint32_t turn = 0;
-  bool lost = false;
-  for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const int64_t b = tile / per, c = ((tile - b * per) * LC + cl) * VEC;
     const bool mine = c < A.channels;
-    const int64_t step = (int64_t)CLT * TB;
-    int64_t t0 = A.len - 1 - (int64_t)rank * TB - group * S;  // of the thread's first step of the walk
+    const int64_t step = TB;
+    int64_t t0 = A.len - 1 - (int64_t)group * S;  // of the thread's first step of the walk
     const T* gate = at<const T>(A.gate, b, t0, c);            // of the round to come
     const T* x = at<const T>(A.x, b, t0, c);
     const T* dh = at<const T>(A.dh, b, t0, c);
@@ -582,7 +512,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
         }
         if (DONE && own) a[i] = kForget;
       }
-      tile_states<VEC, CLT, DONE>(a, m, carry, mu, lcl, rank, turn++, lost, sh);
+      tile_states<VEC, DONE>(a, m, carry, mu, lcl, turn++, sh);
       T* px = dx;
       T* pg = dgate;
 #pragma unroll
@@ -602,7 +532,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
         }
       }
     }
-    if (A.dh0 && mine && rank == 0 && group == 0) {
+    if (A.dh0 && mine && group == 0) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) A.dh0[b * A.channels + c + i] = carry[i];
     }
@@ -619,7 +549,342 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
         const int64_t ch = (tile - b * per) * LC * VEC + j;
         float v = 0.0f;
         for (int w = 0; w < (int)blockDim.x / 32; ++w) v = __fadd_rn(v, reinterpret_cast<const float*>(sh.table[0][w][0])[j]);
-        if (ch < A.channels) part[(b * CLT + rank) * A.channels + ch] = v;
+        if (ch < A.channels) part[b * A.channels + ch] = v;
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Wide tiles: 64 channels, 16 lanes of 4 each, in aligned tensors.
+// The same tile of steps in registers, with the joining done across the block instead of by every thread
+// for itself: the maps of all groups of lanes go to a table, where each thread takes 4 groups of one
+// channel (NW / 2 neighbouring lanes per channel), joins them, and writes back the state before each
+// group.  That is a tenth of the instructions (the tile above takes 11 per element for it, of 40), for a
+// second barrier a round.  Where there are few tiles and many steps, a cluster of blocks shares the steps:
+// per round each block takes its part, in rank order, and posts its map to all others.
+// ---------------------------------------------------------------------------
+constexpr int kWideLanes = 16, kWideChannels = 64, kWidePitch = 68;
+constexpr int kMaxCluster = 8;
+
+template <int NW, int CLT>
+struct WideShared {
+  float4 a[2 * NW * kWidePitch / 4], b[2 * NW * kWidePitch / 4];  // [group][channel]; a also takes the states
+  float2 peer[2][CLT][kWideChannels];                             // [parity][rank]: {A, B}
+  uint64_t bar[2];
+};
+
+// Per thread: its channel and the groups it joins.
+template <int NW>
+struct Joiner {
+  static constexpr int TPC = NW / 2;  // threads per channel, 4 groups each
+  int ch, q;
+  __device__ __forceinline__ Joiner() : ch((int)threadIdx.x / TPC), q((int)threadIdx.x % TPC) {}
+};
+
+// On entry A, B are the thread's map and carry the state of the joiner's channel before the round; on
+// return s is the state before the thread's first step, and carry that after the round.
+template <int NW, int CLT, bool FORGET>
+__device__ __forceinline__ void wide_states(const float (&A)[4], const float (&B)[4], float& carry, float (&s)[4],
+                                            uint32_t rank, uint32_t turn, bool& lost, WideShared<NW, CLT>& sh) {
+  const Joiner<NW> J;
+  constexpr int TPC = Joiner<NW>::TPC;
+  const int group = (int)threadIdx.x / kWideLanes, cl = (int)threadIdx.x % kWideLanes;
+  sh.a[group * (kWidePitch / 4) + cl] = make_float4(A[0], A[1], A[2], A[3]);
+  sh.b[group * (kWidePitch / 4) + cl] = make_float4(B[0], B[1], B[2], B[3]);
+  __syncthreads();
+  float* ta = reinterpret_cast<float*>(sh.a) + 4 * J.q * kWidePitch + J.ch;
+  const float* tb = reinterpret_cast<const float*>(sh.b) + 4 * J.q * kWidePitch + J.ch;
+  float a[4], b[4], ja = 1.0f, jb = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    a[j] = ta[j * kWidePitch];
+    b[j] = tb[j * kWidePitch];
+    float na = a[j], nb = b[j];
+    compose<FORGET>(ja, jb, na, nb);
+    ja = na;
+    jb = nb;
+  }
+#pragma unroll
+  for (int d = 1; d < TPC; d *= 2) {  // the joined maps up to this lane's
+    const float qa = __shfl_up_sync(0xffffffffu, ja, d), qb = __shfl_up_sync(0xffffffffu, jb, d);
+    if (J.q >= d) compose<FORGET>(qa, qb, ja, jb);
+  }
+  float pa = __shfl_up_sync(0xffffffffu, ja, 1), pb = __shfl_up_sync(0xffffffffu, jb, 1);  // and before it
+  if (J.q == 0) {
+    pa = 1.0f;
+    pb = 0.0f;
+  }
+  const int top = ((int)threadIdx.x & 31) | (TPC - 1);
+  ja = __shfl_sync(0xffffffffu, ja, top);  // the block's
+  jb = __shfl_sync(0xffffffffu, jb, top);
+  float in = carry;
+  if (CLT == 1) {
+    carry = apply<FORGET>(ja, jb, carry);
+  } else {
+    // A block may post a round while another still reads the one before, but not the one after: that takes
+    // the other's post of this round.
+    const int parity = (int)(turn & 1u);
+    uint64_t* bar = &sh.bar[parity];
+    if (threadIdx.x == 0) tcx::mbar_arrive_expect_tx(bar, (uint32_t)(8 * kWideChannels * CLT));
+    for (int r = J.q; r < CLT; r += TPC) post_peer(&sh.peer[parity][rank][J.ch], bar, (uint32_t)r, make_float2(ja, jb));
+    lost = lost || !tcx::mbar_wait(bar, (turn >> 1) & 1u, kPeerCycles);
+#pragma unroll
+    for (int r = 0; r < CLT; ++r) {
+      const float2 m = sh.peer[parity][r][J.ch];
+      if (r == (int)rank) in = carry;
+      carry = apply<FORGET>(m.x, m.y, carry);
+    }
+    if (lost) in = carry = nan();  // a post that never came: what the cluster still computes is NaN
+  }
+  float v = J.q == 0 ? in : apply<FORGET>(pa, pb, in);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    ta[j * kWidePitch] = v;
+    v = apply<FORGET>(a[j], b[j], v);
+  }
+  __syncthreads();
+  const float4 o = sh.a[group * (kWidePitch / 4) + cl];
+  s[0] = o.x;
+  s[1] = o.y;
+  s[2] = o.z;
+  s[3] = o.w;
+}
+
+template <int NW, int CLT>
+__device__ __forceinline__ void wide_start(WideShared<NW, CLT>& sh) {
+  if (CLT > 1) {  // every block runs, its barriers ready, before another one posts to it
+    if (threadIdx.x < 2) tcx::mbar_init(&sh.bar[threadIdx.x], 1);
+    tcx::mbar_fence_init();
+    cluster_sync();
+  }
+}
+// Bit k of the group's steps, from the byte of lane k of its 16.
+__device__ __forceinline__ uint32_t group_bits(uint8_t byte) {
+  return __ballot_sync(0xffffffffu, byte != 0) >> ((int)threadIdx.x & 16) & 0xFFFFu;
+}
+
+template <class T, bool DONE, int CLT>
+__global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles) {
+  constexpr int S = kTileSteps, NW = 8, TB = 2 * NW * S;
+  constexpr int64_t step = (int64_t)CLT * TB;
+  extern __shared__ uint4 slots[];
+  __shared__ WideShared<NW, CLT> sh;
+  const int cl = (int)threadIdx.x % kWideLanes, group = (int)threadIdx.x / kWideLanes;
+  const uint32_t rank = CLT == 1 ? 0u : cluster_rank();
+  const Joiner<NW> J;
+  wide_start(sh);
+  const int64_t per = (A.channels + kWideChannels - 1) / kWideChannels;
+  const int64_t rounds = (A.len + step - 1) / step;
+  Ahead<T, 4, 2, S> in;
+  in.start(slots);
+  uint32_t turn = 0;
+  bool lost = false;
+  for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
+    const int64_t b = tile / per, c0 = (tile - b * per) * kWideChannels, c = c0 + 4 * cl;
+    const bool mine = c < A.channels, joins = c0 + J.ch < A.channels;
+    int64_t t0 = (int64_t)rank * TB + group * S;
+    const T* gate = at<const T>(A.gate, b, t0, c);  // of the round to come
+    const T* x = at<const T>(A.x, b, t0, c);
+    T* h = at<T>(A.h, b, t0, c);                    // of the round at hand
+    uint8_t next = 0;                               // of the round to come: done at step t0 + cl - 1
+    const auto bring = [&](int64_t u) {
+      if (mine && u + S <= A.len) {
+        in.bring_all(0, gate, A.gate.st);
+        in.bring_all(1, x, A.x.st);
+      } else if (mine) {
+#pragma unroll 1
+        for (int k = 0; k < S && u + k < A.len; ++k) {
+          in.bring(0, k, gate + k * A.gate.st);
+          in.bring(1, k, x + k * A.x.st);
+        }
+      }
+      copy_commit();
+      gate += step * A.gate.st;
+      x += step * A.x.st;
+      if (DONE) next = u + cl > 0 && u + cl <= A.len && cl < S ? done_byte(A, b, u + cl - 1) : (uint8_t)0;
+    };
+    bring(t0);
+    float bias[4] = {}, carry = joins && A.h0 ? A.h0[b * A.channels + c0 + J.ch] : 0.0f;
+    if (mine) load_bias<4>(A.bias, c, bias);
+    for (int64_t round = 0; round < rounds; ++round, t0 += step, h += step * A.h.st) {
+      float bt[S][4], xt[S][4], a[4], s[4], st[4];
+      const bool whole = mine && t0 + S <= A.len;
+      copy_wait_all();
+      const uint32_t resets = DONE ? group_bits(next) : 0u;  // bit k: the state before step k is dropped
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        float g[4];
+        in.take(0, k, g);
+        in.take(1, k, xt[k]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bt[k][i] = sigmoid_neg(__fmaf_rn(g[i], kLog2e, bias[i]));
+      }
+      if (!whole) {  // steps past the end leave the state as it is
+#pragma unroll
+        for (int k = 0; k < S; ++k)
+          if (!mine || t0 + k >= A.len)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bt[k][i] = xt[k][i] = 0.0f;
+      }
+      if (round + 1 < rounds) bring(t0 + step);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[i] = 1.0f;
+        s[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < S; ++k) {
+          if (DONE && (resets >> k & 1u)) s[i] = 0.0f;
+          s[i] = __fmaf_rn(bt[k][i], __fsub_rn(xt[k][i], s[i]), s[i]);
+          a[i] = __fmaf_rn(-bt[k][i], a[i], a[i]);
+        }
+        if (DONE && resets) a[i] = kForget;
+      }
+      wide_states<NW, CLT, DONE>(a, s, carry, st, rank, turn++, lost, sh);
+      T* p = h;
+#pragma unroll
+      for (int k = 0; k < S; ++k, p += A.h.st) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (DONE && (resets >> k & 1u)) st[i] = 0.0f;
+          st[i] = __fmaf_rn(bt[k][i], __fsub_rn(xt[k][i], st[i]), st[i]);
+        }
+        if (whole || (mine && t0 + k < A.len)) store_vec(p, st);
+      }
+    }
+    if (CLT > 1 && A.h_last == A.h0) cluster_sync();  // h_last in place of h0, which every block has used by now
+    if (A.h_last && joins && rank == 0 && J.q == 0)
+      A.h_last[b * A.channels + c0 + J.ch] = DONE && done_at(A, b, A.len - 1) ? 0.0f : carry;
+  }
+  if (CLT > 1) cluster_sync();  // none leaves while another one may post to it
+}
+
+// Backward, on the steps in reverse order; part [batch * CLT][channels]: sums of dgate (or null).
+template <class T, bool DONE, int CLT>
+__global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t tiles, float* part) {
+  constexpr int S = kTileSteps, NW = 4, TB = 2 * NW * S;
+  constexpr int64_t step = (int64_t)CLT * TB;
+  extern __shared__ uint4 slots[];
+  __shared__ WideShared<NW, CLT> sh;
+  const int cl = (int)threadIdx.x % kWideLanes, group = (int)threadIdx.x / kWideLanes;
+  const uint32_t rank = CLT == 1 ? 0u : cluster_rank();
+  const Joiner<NW> J;
+  pdl_trigger();
+  wide_start(sh);
+  const int64_t per = (A.channels + kWideChannels - 1) / kWideChannels;
+  const int64_t rounds = (A.len + step - 1) / step;
+  Ahead<T, 4, 4, S> in;
+  in.start(slots);
+  uint32_t turn = 0;
+  bool lost = false;
+  for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
+    const int64_t b = tile / per, c0 = (tile - b * per) * kWideChannels, c = c0 + 4 * cl;
+    const bool mine = c < A.channels, joins = c0 + J.ch < A.channels;
+    int64_t t0 = A.len - 1 - (int64_t)rank * TB - group * S;  // of the thread's first step of the walk
+    const T* gate = at<const T>(A.gate, b, t0, c);            // of the round to come
+    const T* x = at<const T>(A.x, b, t0, c);
+    const T* dh = at<const T>(A.dh, b, t0, c);
+    const T* h = at<const T>(A.h, b, t0 - 1, c);
+    T* dx = at<T>(A.dx, b, t0, c);                            // of the round at hand
+    T* dgate = at<T>(A.dgate, b, t0, c);
+    uint8_t next = 0;                                         // of the round to come: done at step t0 - cl
+    const auto bring = [&](int64_t u) {
+      if (mine && u >= S) {
+        in.bring_all(0, gate, -A.gate.st);
+        in.bring_all(1, x, -A.x.st);
+        in.bring_all(2, dh, -A.dh.st);
+        in.bring_all(3, h, -A.h.st);
+      } else if (mine) {
+#pragma unroll 1
+        for (int k = 0; k < S && u - k >= 0; ++k) {
+          in.bring(0, k, gate - k * A.gate.st);
+          in.bring(1, k, x - k * A.x.st);
+          in.bring(2, k, dh - k * A.dh.st);
+          if (u - k > 0) in.bring(3, k, h - k * A.h.st);
+        }
+      }
+      copy_commit();
+      gate -= step * A.gate.st;
+      x -= step * A.x.st;
+      dh -= step * A.dh.st;
+      h -= step * A.h.st;
+      if (DONE) next = u - cl >= 0 && cl <= S ? done_byte(A, b, u - cl) : (uint8_t)0;
+    };
+    bring(t0);
+    float bias[4] = {}, db[4] = {}, carry = joins && A.dh_last ? A.dh_last[b * A.channels + c0 + J.ch] : 0.0f;
+    if (mine) load_bias<4>(A.bias, c, bias);
+    for (int64_t round = 0; round < rounds; ++round, t0 -= step, dx -= step * A.dx.st, dgate -= step * A.dgate.st) {
+      float bt[S][4], qt[S][4], dt[S][4], a[4], m[4], mu[4];  // 1 - a; a (1 - a) (s - x); dh
+      const bool whole = mine && t0 >= S;
+      copy_wait_all();
+      const uint32_t ends = DONE ? group_bits(next) : 0u;  // bit k: done at the walk's step k, S: behind them
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        float g[4], xv[4], s[4];
+        in.take(0, k, g);
+        in.take(1, k, xv);
+        in.take(2, k, dt[k]);
+        in.take(3, k, s);
+        const bool fresh = DONE && (ends >> (k + 1) & 1u);
+        if (!whole && mine && t0 == k) load_row<4>(A.h0, b * A.channels + c, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const Gate q = gate_of(__fmaf_rn(g[i], kLog2e, bias[i]));
+          bt[k][i] = q.b;
+          qt[k][i] = __fmul_rn(q.ab, __fsub_rn(fresh ? 0.0f : s[i], xv[i]));
+        }
+      }
+      if (!whole) {  // steps before the first leave what comes to them as it is
+#pragma unroll
+        for (int k = 0; k < S; ++k)
+          if (!mine || t0 < k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bt[k][i] = qt[k][i] = dt[k][i] = 0.0f;
+      }
+      if (round + 1 < rounds) bring(t0 - step);
+      const uint32_t own = ends & ((1u << S) - 1u);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[i] = 1.0f;
+        m[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < S; ++k) {
+          const float lam = DONE && (own >> k & 1u) ? dt[k][i] : __fadd_rn(dt[k][i], m[i]);
+          m[i] = __fmaf_rn(-bt[k][i], lam, lam);
+          a[i] = __fmaf_rn(-bt[k][i], a[i], a[i]);
+        }
+        if (DONE && own) a[i] = kForget;
+      }
+      wide_states<NW, CLT, DONE>(a, m, carry, mu, rank, turn++, lost, sh);
+      T* px = dx;
+      T* pg = dgate;
+#pragma unroll
+      for (int k = 0; k < S; ++k, px -= A.dx.st, pg -= A.dgate.st) {
+        float ox[4], og[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float lam = DONE && (own >> k & 1u) ? dt[k][i] : __fadd_rn(dt[k][i], mu[i]);
+          ox[i] = __fmul_rn(bt[k][i], lam);
+          og[i] = __fmul_rn(qt[k][i], lam);
+          db[i] = __fadd_rn(db[i], og[i]);  // steps that are not there: qt is 0
+          mu[i] = __fmaf_rn(-bt[k][i], lam, lam);
+        }
+        if (whole || (mine && t0 >= k)) {
+          store_vec(px, ox);
+          store_vec(pg, og);
+        }
+      }
+    }
+    if (A.dh0 && joins && rank == 0 && J.q == 0) A.dh0[b * A.channels + c0 + J.ch] = carry;
+    if (part) {  // the block's sums of its steps, group by group
+      __syncthreads();
+      sh.a[group * (kWidePitch / 4) + cl] = make_float4(db[0], db[1], db[2], db[3]);
+      __syncthreads();
+      if (threadIdx.x < kWideChannels && c0 + threadIdx.x < A.channels) {
+        float v = 0.0f;
+        for (int g = 0; g < 2 * NW; ++g) v = __fadd_rn(v, reinterpret_cast<const float*>(sh.a)[g * kWidePitch + threadIdx.x]);
+        part[(b * CLT + rank) * A.channels + c0 + threadIdx.x] = v;
       }
       __syncthreads();
     }
@@ -648,27 +913,39 @@ __global__ void __launch_bounds__(1024) k_scan_dbias(const float* part, int64_t 
   if (cl == 0 && (int64_t)blockIdx.x * 32 + rl < channels) dbias[(int64_t)blockIdx.x * 32 + rl] = s;
 }
 
-// How a call is cut: lanes per row of channels (log2), warps per block, blocks per cluster.
+// How a call is cut.  columns: up to kColSteps steps.  Wide tiles: aligned tensors of more than 32
+// channels and at least half a block's steps, in clusters of so many blocks; else tiles of 1 << lcl lanes
+// per row of channels and `warps` warps.
 struct ScanPlan {
-  bool columns;
+  bool columns, wide;
   int lcl, warps, cluster;
   int64_t tiles;
 };
-ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, int vec, int max_warps) {
+ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, bool aligned, int max_warps, int per_sm) {
   ScanPlan p{};
   p.columns = len <= kColSteps;
-  const int most = vec == 1 ? 5 : 4;  // 32 or 64 channels
-  while (p.lcl < most && ((int64_t)vec << p.lcl) < channels) ++p.lcl;
-  const int64_t per = (channels + ((int64_t)vec << p.lcl) - 1) / ((int64_t)vec << p.lcl);
-  p.tiles = batch * per;
-  const int64_t steps = (int64_t)(32 >> p.lcl) * kTileSteps;  // per warp
-  p.warps = 1;
-  while (p.warps < max_warps && p.warps * steps < len) p.warps *= 2;
   p.cluster = 1;
-  // clusters post whole vectors of 4 channels
-  const int64_t want = (int64_t)sm_count() * 2;
-  if (vec == 4)
-    while (p.cluster < kMaxCluster && p.warps >= p.cluster * 2 && p.tiles * p.cluster < want && p.warps * steps * p.cluster < len) p.cluster *= 2;
+  const int vec = aligned ? 4 : 1;
+  const int64_t block = (int64_t)max_warps * 2 * kTileSteps;  // a wide block's steps
+  p.wide = !p.columns && aligned && channels > 32 && 2 * len >= block;
+  while (p.lcl < (aligned ? 4 : 5) && ((int64_t)vec << p.lcl) < channels) ++p.lcl;
+  const int64_t width = p.wide ? kWideChannels : (int64_t)vec << p.lcl;
+  p.tiles = batch * ((channels + width - 1) / width);
+  p.warps = 1;
+  while (p.warps < max_warps && p.warps * (int64_t)(32 >> p.lcl) * kTileSteps < len) p.warps *= 2;
+  if (p.wide) {
+    // The cluster that ends first: waves of blocks over the GPU, each 1 / cluster of the steps, and a tenth
+    // more for the posts.
+    const int64_t slots = (int64_t)sm_count() * per_sm;
+    double best = 0.0;
+    for (int cl = 1; cl <= kMaxCluster && (cl == 1 || block * cl <= len); cl *= 2) {
+      const double cost = (double)((p.tiles * cl + slots - 1) / slots) / cl * (cl > 1 ? 1.1 : 1.0);
+      if (cl == 1 || cost < best * 0.99) {
+        best = cost;
+        p.cluster = cl;
+      }
+    }
+  }
   return p;
 }
 
@@ -679,14 +956,14 @@ bool vectors(const simx_scan& a, const simx_seq& q) {
 }
 
 template <class K, class... Args>
-cudaError_t launch_tiles(K* kernel, const ScanPlan& p, size_t smem, cudaStream_t s, Args... args) {
-  cudaError_t e = allow_smem(kernel, 128 * 1024);
+cudaError_t launch_tiles(K* kernel, const ScanPlan& p, int threads, size_t smem, cudaStream_t s, Args... args) {
+  cudaError_t e = allow_smem(kernel, 64 * 1024);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   cudaLaunchAttribute at[1];
   const int64_t teams = std::min<int64_t>(p.tiles, (int64_t)1 << 24);
   lc.gridDim = dim3((unsigned)(teams * p.cluster));
-  lc.blockDim = dim3((unsigned)(p.warps * 32));
+  lc.blockDim = dim3((unsigned)threads);
   lc.dynamicSmemBytes = smem;
   lc.stream = s;
   if (p.cluster > 1) {
@@ -700,33 +977,41 @@ cudaError_t launch_tiles(K* kernel, const ScanPlan& p, size_t smem, cudaStream_t
   return cudaLaunchKernelEx(&lc, kernel, args...);
 }
 
-template <class T, int VEC, bool DONE>
-cudaError_t scan_tiles(const simx_scan& a, const ScanPlan& p, cudaStream_t s) {
-  const size_t smem = VEC == 1 ? 0 : (size_t)p.warps * 32 * 2 * kTileSteps * VEC * sizeof(T);
-  if (VEC > 1) {
-    if (p.cluster == 2) return launch_tiles(k_scan_tiles<T, 4, DONE, 2>, p, smem, s, a, p.lcl, p.tiles);
-    if (p.cluster == 4) return launch_tiles(k_scan_tiles<T, 4, DONE, 4>, p, smem, s, a, p.lcl, p.tiles);
-    if (p.cluster == 8) return launch_tiles(k_scan_tiles<T, 4, DONE, 8>, p, smem, s, a, p.lcl, p.tiles);
-  }
-  return launch_tiles(k_scan_tiles<T, VEC, DONE, 1>, p, smem, s, a, p.lcl, p.tiles);
-}
-template <class T, int VEC, bool DONE>
-cudaError_t scan_grad_tiles(const simx_scan& a, const ScanPlan& p, float* part, cudaStream_t s) {
-  const size_t smem = VEC == 1 ? 0 : (size_t)p.warps * 32 * 4 * kTileSteps * VEC * sizeof(T);
-  if (VEC > 1) {
-    if (p.cluster == 2) return launch_tiles(k_scan_grad_tiles<T, 4, DONE, 2>, p, smem, s, a, p.lcl, p.tiles, part);
-    if (p.cluster == 4) return launch_tiles(k_scan_grad_tiles<T, 4, DONE, 4>, p, smem, s, a, p.lcl, p.tiles, part);
-    if (p.cluster == 8) return launch_tiles(k_scan_grad_tiles<T, 4, DONE, 8>, p, smem, s, a, p.lcl, p.tiles, part);
-  }
-  return launch_tiles(k_scan_grad_tiles<T, VEC, DONE, 1>, p, smem, s, a, p.lcl, p.tiles, part);
-}
+constexpr int kFwdWarps = 8, kFwdPerSm = 2, kGradWarps = 4, kGradPerSm = 3;
 
-constexpr int kFwdWarps = 8, kGradWarps = 4;
+template <class T, bool DONE>
+cudaError_t scan_tiles(const simx_scan& a, const ScanPlan& p, bool v4, cudaStream_t s) {
+  if (p.wide) {
+    const int th = 32 * kFwdWarps;
+    const size_t smem = (size_t)th * 2 * kTileSteps * 4 * sizeof(T);
+    if (p.cluster == 8) return launch_tiles(k_scan_wide<T, DONE, 8>, p, th, smem, s, a, p.tiles);
+    if (p.cluster == 4) return launch_tiles(k_scan_wide<T, DONE, 4>, p, th, smem, s, a, p.tiles);
+    if (p.cluster == 2) return launch_tiles(k_scan_wide<T, DONE, 2>, p, th, smem, s, a, p.tiles);
+    return launch_tiles(k_scan_wide<T, DONE, 1>, p, th, smem, s, a, p.tiles);
+  }
+  const size_t smem = (size_t)p.warps * 32 * 2 * kTileSteps * 4 * sizeof(T);
+  if (v4) return launch_tiles(k_scan_tiles<T, 4, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles);
+  return launch_tiles(k_scan_tiles<T, 1, DONE>, p, 32 * p.warps, 0, s, a, p.lcl, p.tiles);
+}
+template <class T, bool DONE>
+cudaError_t scan_grad_tiles(const simx_scan& a, const ScanPlan& p, bool v4, float* part, cudaStream_t s) {
+  if (p.wide) {
+    const int th = 32 * kGradWarps;
+    const size_t smem = (size_t)th * 4 * kTileSteps * 4 * sizeof(T);
+    if (p.cluster == 8) return launch_tiles(k_scan_grad_wide<T, DONE, 8>, p, th, smem, s, a, p.tiles, part);
+    if (p.cluster == 4) return launch_tiles(k_scan_grad_wide<T, DONE, 4>, p, th, smem, s, a, p.tiles, part);
+    if (p.cluster == 2) return launch_tiles(k_scan_grad_wide<T, DONE, 2>, p, th, smem, s, a, p.tiles, part);
+    return launch_tiles(k_scan_grad_wide<T, DONE, 1>, p, th, smem, s, a, p.tiles, part);
+  }
+  const size_t smem = (size_t)p.warps * 32 * 4 * kTileSteps * 4 * sizeof(T);
+  if (v4) return launch_tiles(k_scan_grad_tiles<T, 4, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles, part);
+  return launch_tiles(k_scan_grad_tiles<T, 1, DONE>, p, 32 * p.warps, 0, s, a, p.lcl, p.tiles, part);
+}
 
 template <class T>
 cudaError_t scan(const simx_scan& a, cudaStream_t s) {
   const bool v4 = a.channels % 4 == 0 && (a.len == 0 || (vectors<T>(a, a.x) && vectors<T>(a, a.gate) && vectors<T>(a, a.h)));
-  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4 ? 4 : 1, kFwdWarps);
+  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4, kFwdWarps, kFwdPerSm);
   if (p.columns) {
     const int64_t cols = a.batch * (v4 ? a.channels / 4 : a.channels);
     const unsigned blocks = (unsigned)((cols + kColThreads - 1) / kColThreads);
@@ -735,16 +1020,15 @@ cudaError_t scan(const simx_scan& a, cudaStream_t s) {
     count_launches(1);
     return cudaGetLastError();
   }
-  if (v4) return a.done ? scan_tiles<T, 4, true>(a, p, s) : scan_tiles<T, 4, false>(a, p, s);
-  return a.done ? scan_tiles<T, 1, true>(a, p, s) : scan_tiles<T, 1, false>(a, p, s);
+  return a.done ? scan_tiles<T, true>(a, p, v4, s) : scan_tiles<T, false>(a, p, v4, s);
 }
 
 template <class T>
 cudaError_t scan_grad(const simx_scan& a, float* part, int64_t& rows, cudaStream_t s) {
   const bool v4 = a.channels % 4 == 0 && (a.len == 0 || (vectors<T>(a, a.x) && vectors<T>(a, a.gate) && vectors<T>(a, a.h) &&
                                                          vectors<T>(a, a.dh) && vectors<T>(a, a.dx) && vectors<T>(a, a.dgate)));
-  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4 ? 4 : 1, kGradWarps);
-  rows = a.batch * (p.columns ? 1 : p.cluster);
+  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4, kGradWarps, kGradPerSm);
+  rows = a.batch * p.cluster;
   if (p.columns) {
     const int64_t cols = a.batch * (v4 ? a.channels / 4 : a.channels);
     const unsigned blocks = (unsigned)((cols + kColThreads - 1) / kColThreads);
@@ -753,8 +1037,7 @@ cudaError_t scan_grad(const simx_scan& a, float* part, int64_t& rows, cudaStream
     count_launches(1);
     return cudaGetLastError();
   }
-  if (v4) return a.done ? scan_grad_tiles<T, 4, true>(a, p, part, s) : scan_grad_tiles<T, 4, false>(a, p, part, s);
-  return a.done ? scan_grad_tiles<T, 1, true>(a, p, part, s) : scan_grad_tiles<T, 1, false>(a, p, part, s);
+  return a.done ? scan_grad_tiles<T, true>(a, p, v4, part, s) : scan_grad_tiles<T, false>(a, p, v4, part, s);
 }
 
 }  // namespace
@@ -762,8 +1045,8 @@ cudaError_t scan_grad(const simx_scan& a, float* part, int64_t& rows, cudaStream
 // The backward pass's sums of dgate: a row of channels per batch entry and block of a cluster (the plan of
 // aligned tensors, whose clusters may be larger than one).
 size_t scan_workspace_bytes(int64_t batch, int64_t len, int64_t channels) {
-  const ScanPlan p = plan_scan(batch, len, channels, 4, kGradWarps);
-  return (size_t)batch * (size_t)(p.columns ? 1 : p.cluster) * (size_t)channels * sizeof(float);
+  const ScanPlan p = plan_scan(batch, len, channels, true, kGradWarps, kGradPerSm);
+  return (size_t)batch * (size_t)p.cluster * (size_t)channels * sizeof(float);
 }
 
 cudaError_t launch_scan(const simx_scan& a, cudaStream_t s) {
