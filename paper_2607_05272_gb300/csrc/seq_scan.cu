@@ -892,25 +892,9 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
   if (CLT > 1) cluster_sync();
 }
 
-// dbias[c] = the sum over the rows of part [rows][channels]: 32 channels per block, 32 rows at a time,
-// joined in a fixed order.
 __global__ void __launch_bounds__(1024) k_scan_dbias(const float* part, int64_t rows, int64_t channels, float* dbias) {
-  __shared__ float sh[32][33];
-  const int cl = threadIdx.x & 31, rl = (int)threadIdx.x / 32;
-  const int64_t c = (int64_t)blockIdx.x * 32 + cl;
   pdl_wait();
-  float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (c < channels) {
-    int64_t r = rl;
-    for (; r + 96 < rows; r += 128)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = __fadd_rn(v[u], part[(r + 32 * u) * channels + c]);
-    for (; r < rows; r += 32) v[0] = __fadd_rn(v[0], part[r * channels + c]);
-  }
-  sh[rl][cl] = __fadd_rn(__fadd_rn(v[0], v[1]), __fadd_rn(v[2], v[3]));
-  __syncthreads();
-  const float s = sum_lanes(sh[cl][rl]);
-  if (cl == 0 && (int64_t)blockIdx.x * 32 + rl < channels) dbias[(int64_t)blockIdx.x * 32 + rl] = s;
+  column_sums(part, rows, channels, (int64_t)blockIdx.x * 32, dbias);
 }
 
 // How a call is cut.  columns: up to kColSteps steps.  Wide tiles: aligned tensors of more than 32
