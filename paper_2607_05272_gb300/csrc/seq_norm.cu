@@ -70,55 +70,70 @@ __device__ __forceinline__ Raw<__nv_bfloat16> raw_of(const float (&v)[8], __nv_b
   return r;
 }
 
+// One unit of a row element by element, zeros outside of it.
+template <class T>
+__device__ __noinline__ Raw<T> load_slow(const T* p, int c0, int width) {
+  float f[kUnit];
+#pragma unroll
+  for (int j = 0; j < kUnit; ++j) f[j] = c0 + j >= 0 && c0 + j < width ? widen(p[c0 + j]) : 0.0f;
+  return raw_of(f, T());
+}
+template <class T>
+__device__ __noinline__ void store_slow(T* p, int c0, int width, Raw<T> r) {
+#pragma unroll
+  for (int j = 0; j < kUnit; ++j)
+    if (c0 + j >= 0 && c0 + j < width) p[c0 + j] = narrow<T>(elem(r, j));
+}
+
 // A row of a tensor on the grid of units: unit v holds columns 8 v - ph .. 8 v - ph + 7, ph the elements
 // between a 16-byte boundary and the row that gives the grid.  on_grid: this tensor's row lies on it too.
+// A partial unit is loaded whole all the same (what lies beside the row belongs to the rows next to it)
+// and masked, except where it would leave the tensor.
 // AL: every row of every tensor is aligned and the width a multiple of 8.
 template <class T, bool AL>
 struct Row {
   T* p;
   bool on_grid;
-  __device__ __forceinline__ Row(const void* base, int64_t row, int64_t ld, int ph)
-      : p(const_cast<T*>(static_cast<const T*>(base)) + (base ? row * ld : 0)), on_grid(AL || phase(p) == ph) {}
+  int64_t before, after;  // elements of the tensor before the row, and from its start on
+  __device__ __forceinline__ Row(const void* base, int64_t row, int64_t ld, int ph, int64_t n, int width)
+      : p(const_cast<T*>(static_cast<const T*>(base)) + (base ? row * ld : 0)),
+        on_grid(AL || phase(p) == ph), before(row * ld), after((n - 1 - row) * ld + width) {}
   static __device__ __forceinline__ int phase(const T* p) { return (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T)); }
   __device__ __forceinline__ Raw<T> load(int v, int ph, int width) const {
-    Raw<T> r;
-    if (AL || (on_grid && v * kUnit >= ph && v * kUnit - ph + kUnit <= width)) {
-      const uint4* g = reinterpret_cast<const uint4*>(p - ph) + v * Raw<T>::Q;
+    const int c0 = v * kUnit - ph;
+    if (AL || (on_grid && c0 + before >= 0 && c0 + kUnit <= after)) {
+      Raw<T> r;
+      const uint4* g = reinterpret_cast<const uint4*>(p + c0);
 #pragma unroll
       for (int i = 0; i < Raw<T>::Q; ++i) r.q[i] = g[i];
-    } else {
-      float f[kUnit];
-#pragma unroll
-      for (int j = 0; j < kUnit; ++j) {
-        const int c = v * kUnit - ph + j;
-        f[j] = c >= 0 && c < width ? widen(p[c]) : 0.0f;
-      }
-      r = raw_of(f, T());
+      return r;
     }
-    return r;
+    return load_slow(static_cast<const T*>(p), c0, width);
   }
   __device__ __forceinline__ void store(int v, int ph, int width, const float (&f)[kUnit]) const {
-    if (AL || (on_grid && v * kUnit >= ph && v * kUnit - ph + kUnit <= width)) {
-      const Raw<T> r = raw_of(f, T());
-      uint4* g = reinterpret_cast<uint4*>(p - ph) + v * Raw<T>::Q;
+    const int c0 = v * kUnit - ph;
+    const Raw<T> r = raw_of(f, T());
+    if (AL || (on_grid && c0 >= 0 && c0 + kUnit <= width)) {
+      uint4* g = reinterpret_cast<uint4*>(p + c0);
 #pragma unroll
       for (int i = 0; i < Raw<T>::Q; ++i) __stcs(g + i, r.q[i]);
     } else {
-#pragma unroll
-      for (int j = 0; j < kUnit; ++j) {
-        const int c = v * kUnit - ph + j;
-        if (c >= 0 && c < width) p[c] = narrow<T>(f[j]);
-      }
+      store_slow(p, c0, width, r);
     }
   }
 };
 
-// Place of column c in a shared array that lanes read at a distance of 8: one word of padding per 32.
-__device__ __forceinline__ int padded(int c) { return c + (c >> 5); }
+// Shared arrays over columns, for rows off the grid: column c in plane c % 8 at c / 8 + 1, so that lanes
+// with neighbouring units read neighbouring words whatever the phase; places before and behind the row
+// hold zeros.  Element j of unit v of phase ph is at plane_of(j, ph, pitch) + v.
+__device__ __forceinline__ int plane_pitch(int width) { return width / kUnit + 4; }
+__device__ __forceinline__ int plane_of(int j, int ph, int pitch) {
+  return ((j - ph) & 7) * pitch + (j < ph ? 0 : 1);
+}
 
-// The gains of unit v: from the caches, or from shared memory where columns lie across vectors.
+// The gains of unit v: from the caches, or from shared memory.
 template <bool AL>
-__device__ __forceinline__ void gains(const float* gain, const float* sh, int v, int ph, int width, float (&w)[kUnit]) {
+__device__ __forceinline__ void gains(const float* gain, const float* sh, int v, int ph, int pitch, float (&w)[kUnit]) {
   if (AL) {
     const float4 a = __ldg(reinterpret_cast<const float4*>(gain) + 2 * v), b = __ldg(reinterpret_cast<const float4*>(gain) + 2 * v + 1);
     const float q[kUnit] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -126,22 +141,27 @@ __device__ __forceinline__ void gains(const float* gain, const float* sh, int v,
     for (int j = 0; j < kUnit; ++j) w[j] = q[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) {
-      const int c = v * kUnit - ph + j;
-      w[j] = c >= 0 && c < width ? sh[padded(c)] : 0.0f;
-    }
+    for (int j = 0; j < kUnit; ++j) w[j] = sh[plane_of(j, ph, pitch) + v];
+  }
+}
+__device__ __forceinline__ void fill_gains(const float* gain, float* sh, int width) {
+  const int pitch = plane_pitch(width);
+  for (int i = threadIdx.x; i < kUnit * pitch; i += blockDim.x) {
+    const int c = (i % pitch - 1) * kUnit + i / pitch;
+    sh[i] = c >= 0 && c < width ? gain[c] : 0.0f;
   }
 }
 
 // The keep bits of a warp's units first + 32 i + lane, i < NV, of a row of phase ph.  A unit's columns are
 // the last ph of one group and the first 8 - ph of the next, which the next lane draws.
 template <int NV, bool AL>
-__device__ __forceinline__ void unit_bits(const Drop& D, int first, uint32_t row, int ph, uint32_t (&bits)[NV]) {
+__device__ __forceinline__ void unit_bits(const Drop& D, int first, int units, uint32_t row, int ph, uint32_t (&bits)[NV]) {
   const int lane = threadIdx.x & 31;
   uint32_t before = 0;  // of the unit before the warp's first
   if (!AL && ph != 0 && first > 0) before = keep_bits(D, (uint32_t)(first - 1), row);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
+    if (first + 32 * i >= units) break;  // the same in the whole warp
     const uint32_t own = keep_bits(D, (uint32_t)(first + 32 * i + lane), row);
     bits[i] = own;
     if (!AL && ph != 0) {
@@ -153,48 +173,50 @@ __device__ __forceinline__ void unit_bits(const Drop& D, int first, uint32_t row
   }
 }
 
-// Joins v over the W warps of a row; turn: calls so far (the tables alternate, so that one barrier does).
-template <int W>
+// Joins v over the warps of a row; turn: calls so far (the tables alternate, so that one barrier does).
+template <bool ONE>
 __device__ __forceinline__ float row_sum(float v, int turn, float (&sh)[2][32]) {
   v = sum_lanes(v);
-  if (W == 1) return v;
+  if (ONE) return v;
   const int lane = threadIdx.x & 31;
   if (lane == 0) sh[turn & 1][threadIdx.x / 32] = v;
   __syncthreads();
-  return sum_lanes(lane < W ? sh[turn & 1][lane] : 0.0f);
+  return sum_lanes(lane < (int)blockDim.x / 32 ? sh[turn & 1][lane] : 0.0f);
 }
 
-template <int W>
-constexpr int rows_per_block() {  // narrow rows: a warp each
-  return W == 1 ? 4 : 1;
+constexpr int kRowsOfOne = 4;  // ONE: a warp per row, four to a block; else a block per row
+
+// Threads per SM: 512 with 16 registers of each tensor a thread, twice as many with 8 or fewer.
+template <class T, int NV>
+constexpr int norm_sm_threads() {
+  return NV * (int)sizeof(T) * 2 <= 8 ? 1024 : 512;
 }
-template <int W>
+// Most threads of a block (rows of 17 warps and more: 64 registers a thread), and blocks per SM of them.
+template <bool ONE, bool WIDE>
 constexpr int norm_threads() {
-  return 32 * W * rows_per_block<W>();
+  return ONE ? 32 * kRowsOfOne : WIDE ? 1024 : 512;
+}
+template <class T, bool ONE, int NV, bool WIDE>
+constexpr int norm_blocks_per_sm() {
+  return std::max(1, norm_sm_threads<T, NV>() / norm_threads<ONE, WIDE>());
 }
 
-// Blocks per SM: 512 threads with 16 registers of each tensor a thread, twice as many with 8 or fewer.
-template <class T, int W, int NV>
-constexpr int norm_per_sm() {
-  return std::max(1, (NV * (int)sizeof(T) * 2 <= 8 ? 1024 : 512) / norm_threads<W>());
-}
-
-template <class T, int W, int NV, bool AL>
-__global__ void __launch_bounds__(norm_threads<W>(), (norm_per_sm<T, W, NV>())) k_norm_rows(simx_norm A, Drop D) {
-  constexpr int RB = rows_per_block<W>();
+template <class T, bool ONE, int NV, bool AL, bool WIDE>
+__global__ void __launch_bounds__((norm_threads<ONE, WIDE>()), (norm_blocks_per_sm<T, ONE, NV, WIDE>())) k_norm_rows(simx_norm A, Drop D) {
+  constexpr int RB = ONE ? kRowsOfOne : 1;
   extern __shared__ float gs[];
   __shared__ float sh[2][32];
-  const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32, width = (int)A.width;
-  const int first = (W == 1 ? 0 : warp) * NV * 32;
+  const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32, width = (int)A.width, pitch = plane_pitch(width);
+  const int first = (ONE ? 0 : warp) * NV * 32;
   if (!AL) {
-    for (int c = threadIdx.x; c < width; c += norm_threads<W>()) gs[padded(c)] = A.gain[c];
+    fill_gains(A.gain, gs, width);
     __syncthreads();
   }
   int turn = 0;
-  for (int64_t i = (int64_t)blockIdx.x * RB + (W == 1 ? warp : 0); i < A.n; i += (int64_t)gridDim.x * RB) {
+  for (int64_t i = (int64_t)blockIdx.x * RB + (ONE ? warp : 0); i < A.n; i += (int64_t)gridDim.x * RB) {
     const int ph = AL ? 0 : Row<T, AL>::phase(static_cast<const T*>(A.x) + i * A.x_ld);
     const int units = (ph + width + kUnit - 1) / kUnit;
-    const Row<T, AL> x(A.x, i, A.x_ld, ph), res(A.residual, i, A.residual_ld, ph), z(A.z, i, A.z_ld, ph), y(A.y, i, A.y_ld, ph);
+    const Row<T, AL> x(A.x, i, A.x_ld, ph, A.n, width), res(A.residual, i, A.residual_ld, ph, A.n, width);
     Raw<T> rx[NV], rr[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -207,59 +229,76 @@ __global__ void __launch_bounds__(norm_threads<W>(), (norm_per_sm<T, W, NV>())) 
     uint32_t bits[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) bits[k] = 0xFFu;
-    if (D.thr) unit_bits<NV, AL>(D, first, D.row_base + (uint32_t)i, ph, bits);
+    if (D.thr) unit_bits<NV, AL>(D, first, units, D.row_base + (uint32_t)i, ph, bits);
     float f[NV][kUnit], ss = 0.0f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const bool live = first + 32 * k + lane < units;
+      const int v = first + 32 * k + lane, c0 = v * kUnit - ph;
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) {
         float s = A.residual ? elem(rr[k], j) : 0.0f;
         if (bits[k] >> j & 1u) s = __fmaf_rn(elem(rx[k], j), D.scale, s);
-        f[k][j] = live ? s : 0.0f;  // columns outside the row are zeros too
-        ss = __fmaf_rn(f[k][j], f[k][j], ss);
+        f[k][j] = s;
       }
+      if (v >= units || (!AL && (c0 < 0 || c0 + kUnit > width))) {  // columns outside the row are zeros
+#pragma unroll
+        for (int j = 0; j < kUnit; ++j)
+          if (v >= units || c0 + j < 0 || c0 + j >= width) f[k][j] = 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) ss = __fmaf_rn(f[k][j], f[k][j], ss);
     }
-    ss = row_sum<W>(ss, turn++, sh);
+    ss = row_sum<ONE>(ss, turn++, sh);
     const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)width), A.eps)));
+    const Row<T, AL> z(A.z, i, A.z_ld, ph, A.n, width), y(A.y, i, A.y_ld, ph, A.n, width);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int v = first + 32 * k + lane;
       if (v >= units) continue;
       float w[kUnit], o[kUnit];
-      gains<AL>(A.gain, gs, v, ph, width, w);
+      gains<AL>(A.gain, gs, v, ph, pitch, w);
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) o[j] = __fmul_rn(__fmul_rn(f[k][j], r), w[j]);
       if (A.z) z.store(v, ph, width, f[k]);
       y.store(v, ph, width, o);
     }
-    if (A.rstd && lane == 0 && (W == 1 || warp == 0)) A.rstd[i] = r;
+    if (A.rstd && lane == 0 && (ONE || warp == 0)) A.rstd[i] = r;
   }
 }
 
-// Backward.  slab [gridDim][width]: the block's sums of dy zh (or null), in registers where a thread's
-// columns are the same in every row, else in shared memory (one array per row of the block).
-template <class T, int W, int NV, bool AL>
-__global__ void __launch_bounds__(norm_threads<W>(), (norm_per_sm<T, W, NV>())) k_norm_grad_rows(simx_norm A, Drop D, float* slab) {
-  constexpr int RB = rows_per_block<W>(), THREADS = norm_threads<W>();
+// Zeros the elements of a unit outside the row.
+template <class T>
+__device__ __forceinline__ Raw<T> masked(const Raw<T>& r, int c0, int width) {
+  float f[kUnit];
+#pragma unroll
+  for (int j = 0; j < kUnit; ++j) f[j] = c0 + j >= 0 && c0 + j < width ? elem(r, j) : 0.0f;
+  return raw_of(f, T());
+}
+
+// Backward.  slab [gridDim][width]: the block's sums of dy zh (or null).  Where a thread's columns are the
+// same in every row they are in registers; else in shared memory, an array per warp over its own units and
+// one place before them (which the warp before has too), so that no other warp waits.
+template <class T, bool ONE, int NV, bool AL, bool WIDE>
+__global__ void __launch_bounds__((norm_threads<ONE, WIDE>()), (norm_blocks_per_sm<T, ONE, NV, WIDE>())) k_norm_grad_rows(simx_norm A, Drop D, float* slab) {
+  constexpr int RB = ONE ? kRowsOfOne : 1, SP = NV * 32 + 2;  // pitch of a warp's planes
   extern __shared__ float gs[];
   __shared__ float sh[2][32];
   pdl_trigger();
-  const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32, width = (int)A.width, pitch = padded(width) + 1;
-  const int first = (W == 1 ? 0 : warp) * NV * 32;
-  float* sums = gs + pitch * (1 + (W == 1 ? warp : 0));  // !AL
+  const int lane = threadIdx.x & 31, warp = (int)threadIdx.x / 32, width = (int)A.width, pitch = plane_pitch(width);
+  const int first = (ONE ? 0 : warp) * NV * 32, warps = (int)blockDim.x / 32;
+  float* all = gs + (AL ? 0 : kUnit * pitch);
+  float* sums = all + warp * kUnit * SP;  // !AL
   if (!AL) {
-    for (int c = threadIdx.x; c < width; c += THREADS) gs[padded(c)] = A.gain[c];
-    for (int c = threadIdx.x; c < pitch * RB; c += THREADS) gs[pitch + c] = 0.0f;
+    fill_gains(A.gain, gs, width);
+    for (int c = threadIdx.x; c < warps * kUnit * SP; c += (int)blockDim.x) all[c] = 0.0f;
     __syncthreads();
   }
   float acc[AL ? NV : 1][kUnit] = {};
   int turn = 0;
-  for (int64_t i = (int64_t)blockIdx.x * RB + (W == 1 ? warp : 0); i < A.n; i += (int64_t)gridDim.x * RB) {
+  for (int64_t i = (int64_t)blockIdx.x * RB + (ONE ? warp : 0); i < A.n; i += (int64_t)gridDim.x * RB) {
     const int ph = AL ? 0 : Row<T, AL>::phase(static_cast<const T*>(A.z) + i * A.z_ld);
     const int units = (ph + width + kUnit - 1) / kUnit;
-    const Row<T, AL> z(A.z, i, A.z_ld, ph), dy(A.dy, i, A.dy_ld, ph), dz(A.dz, i, A.dz_ld, ph), dx(A.dx, i, A.dx_ld, ph),
-        dr(A.dresidual, i, A.dresidual_ld, ph);
+    const Row<T, AL> z(A.z, i, A.z_ld, ph, A.n, width), dy(A.dy, i, A.dy_ld, ph, A.n, width), dz(A.dz, i, A.dz_ld, ph, A.n, width);
     const float r = A.rstd[i];
     Raw<T> rz[NV], ry[NV], rd[NV];
 #pragma unroll
@@ -274,14 +313,18 @@ __global__ void __launch_bounds__(norm_threads<W>(), (norm_per_sm<T, W, NV>())) 
     uint32_t bits[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) bits[k] = 0xFFu;
-    if (D.thr && A.dx) unit_bits<NV, AL>(D, first, D.row_base + (uint32_t)i, ph, bits);
+    if (D.thr && A.dx) unit_bits<NV, AL>(D, first, units, D.row_base + (uint32_t)i, ph, bits);
     float dot = 0.0f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int v = first + 32 * k + lane;
+      const int v = first + 32 * k + lane, c0 = v * kUnit - ph;
       if (v >= units) continue;
+      if (!AL && (c0 < 0 || c0 + kUnit > width)) {
+        rz[k] = masked(rz[k], c0, width);
+        ry[k] = masked(ry[k], c0, width);
+      }
       float w[kUnit];
-      gains<AL>(A.gain, gs, v, ph, width, w);
+      gains<AL>(A.gain, gs, v, ph, pitch, w);
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) {
         const float zh = __fmul_rn(elem(rz[k], j), r), d = elem(ry[k], j);
@@ -289,18 +332,19 @@ __global__ void __launch_bounds__(norm_threads<W>(), (norm_per_sm<T, W, NV>())) 
         if (AL) {
           acc[AL ? k : 0][j] = __fmaf_rn(d, zh, acc[AL ? k : 0][j]);
         } else if (slab) {
-          const int c = v * kUnit - ph + j;
-          if (c >= 0 && c < width) sums[padded(c)] = __fmaf_rn(d, zh, sums[padded(c)]);
+          float* s = sums + plane_of(j, ph, SP) + 32 * k + lane;
+          *s = __fmaf_rn(d, zh, *s);
         }
       }
     }
-    const float mean = __fdiv_rn(row_sum<W>(dot, turn++, sh), (float)width);
+    const float mean = __fdiv_rn(row_sum<ONE>(dot, turn++, sh), (float)width);
+    const Row<T, AL> dx(A.dx, i, A.dx_ld, ph, A.n, width), dr(A.dresidual, i, A.dresidual_ld, ph, A.n, width);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int v = first + 32 * k + lane;
       if (v >= units) continue;
       float w[kUnit], o[kUnit];
-      gains<AL>(A.gain, gs, v, ph, width, w);
+      gains<AL>(A.gain, gs, v, ph, pitch, w);
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) {
         const float zh = __fmul_rn(elem(rz[k], j), r);
@@ -314,14 +358,11 @@ __global__ void __launch_bounds__(norm_threads<W>(), (norm_per_sm<T, W, NV>())) 
         dx.store(v, ph, width, o);
       }
     }
-    if (!AL) {  // the next row's columns belong to other threads
-      if (W > 1) __syncthreads();
-      else __syncwarp();
-    }
+    if (!AL) __syncwarp();  // the next row's columns may be other lanes'
   }
   if (!slab) return;
   float* out = slab + (int64_t)blockIdx.x * width;
-  if (AL && W > 1) {
+  if (AL && !ONE) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (first + 32 * k + lane) * kUnit;
@@ -332,7 +373,7 @@ __global__ void __launch_bounds__(norm_threads<W>(), (norm_per_sm<T, W, NV>())) 
     }
     return;
   }
-  if (AL) {  // the block's warps by way of shared memory
+  if (AL) {  // the block's rows by way of shared memory
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (32 * k + lane) * kUnit;
@@ -342,9 +383,17 @@ __global__ void __launch_bounds__(norm_threads<W>(), (norm_per_sm<T, W, NV>())) 
     }
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < width; c += THREADS) {
+  for (int c = threadIdx.x; c < width; c += (int)blockDim.x) {
     float v = 0.0f;
-    for (int q = 0; q < RB; ++q) v = __fadd_rn(v, AL ? gs[q * width + c] : gs[pitch * (1 + q) + padded(c)]);
+    if (AL) {
+      for (int q = 0; q < RB; ++q) v = __fadd_rn(v, gs[q * width + c]);
+    } else if (ONE) {
+      for (int q = 0; q < RB; ++q) v = __fadd_rn(v, all[(q * kUnit + c % kUnit) * SP + c / kUnit + 1]);
+    } else {  // the warp of the column's unit, and the place before the first of the next
+      const int u = c / kUnit, q = u / (NV * 32), l = u % (NV * 32);
+      v = all[(q * kUnit + c % kUnit) * SP + l + 1];
+      if (l == NV * 32 - 1 && q + 1 < warps) v = __fadd_rn(v, all[((q + 1) * kUnit + c % kUnit) * SP]);
+    }
     out[c] = v;
   }
 }
@@ -377,48 +426,51 @@ bool aligned(const simx_norm& a, bool grad) {
   return ok(a.dy, a.dy_ld) && ok(a.dz, a.dz_ld) && ok(a.dx, a.dx_ld) && ok(a.dresidual, a.dresidual_ld);
 }
 
-// Blocks of a launch: at most what the GPU holds at a time, and at most the slabs of dgain.
-int64_t norm_blocks(int64_t n, int warps, int per_sm) {
-  const int rb = warps == 1 ? 4 : 1;
-  return std::min<int64_t>({(n + rb - 1) / rb, (int64_t)sm_count() * per_sm, kMaxSlabs});
-}
-
-template <class T, int W, int NV, bool AL>
-cudaError_t norm_launch(const simx_norm& a, const Drop& d, float* slab, int64_t& slabs, bool grad, cudaStream_t s) {
-  const size_t pitch = (size_t)a.width + (size_t)a.width / 32 + 1;
-  size_t sh = AL ? 0 : pitch * sizeof(float);
-  if (grad) sh = AL ? (W == 1 ? (size_t)a.width * 4 * sizeof(float) : 0) : pitch * (1 + rows_per_block<W>()) * sizeof(float);
-  slabs = norm_blocks(a.n, W, norm_per_sm<T, W, NV>());
+template <class T, bool ONE, int NV, bool AL, bool WIDE>
+cudaError_t norm_launch(const simx_norm& a, const Drop& d, int warps, float* slab, int64_t& slabs, bool grad, cudaStream_t s) {
+  const int threads = 32 * (ONE ? kRowsOfOne : warps);
+  const size_t planes = (size_t)(kUnit * (a.width / kUnit + 4));
+  size_t sh = AL ? 0 : planes * sizeof(float);
+  if (grad) sh = AL ? (ONE ? (size_t)a.width * kRowsOfOne * sizeof(float) : 0) : (planes + (size_t)(threads / 32) * kUnit * (NV * 32 + 2)) * sizeof(float);
+  // as many blocks as the GPU holds at a time, each with rows in turn; the backward pass leaves a slab each
+  const int per_sm = std::max(1, norm_sm_threads<T, NV>() / threads);
+  const int64_t rb = ONE ? kRowsOfOne : 1;
+  slabs = std::min<int64_t>({(a.n + rb - 1) / rb, (int64_t)sm_count() * per_sm, kMaxSlabs});
   cudaError_t e = cudaSuccess;
   if (grad) {
-    if ((e = allow_smem(k_norm_grad_rows<T, W, NV, AL>, 2 * (kNormMaxWidth + kNormMaxWidth / 32 + 1) * (int)sizeof(float))) != cudaSuccess) return e;
-    k_norm_grad_rows<T, W, NV, AL><<<(unsigned)slabs, norm_threads<W>(), sh, s>>>(a, d, slab);
+    const auto kernel = k_norm_grad_rows<T, ONE, NV, AL, WIDE>;
+    if ((e = allow_smem(kernel, 160 * 1024)) != cudaSuccess) return e;
+    kernel<<<(unsigned)slabs, threads, sh, s>>>(a, d, slab);
   } else {
-    if ((e = allow_smem(k_norm_rows<T, W, NV, AL>, (kNormMaxWidth + kNormMaxWidth / 32 + 1) * (int)sizeof(float))) != cudaSuccess) return e;
-    k_norm_rows<T, W, NV, AL><<<(unsigned)slabs, norm_threads<W>(), sh, s>>>(a, d);
+    const auto kernel = k_norm_rows<T, ONE, NV, AL, WIDE>;
+    if ((e = allow_smem(kernel, 80 * 1024)) != cudaSuccess) return e;
+    kernel<<<(unsigned)slabs, threads, sh, s>>>(a, d);
   }
   count_launches(1);
   return cudaGetLastError();
 }
 
-// 16 32-bit registers of each tensor a thread (4 units of bf16, 2 of fp32), and as many warps per row as
-// that takes; fewer units for rows that a warp has room for.
+// Units per thread and warps per row: up to 16 32-bit registers of each tensor a thread (4 units of bf16, 2 of
+// fp32); a warp per row where that has room, else the count of units that leaves the fewest places empty
+// (rows off the 16-byte grid lie on one unit more).
 template <class T, bool AL>
 cudaError_t norm_rows(const simx_norm& a, const Drop& d, float* slab, int64_t& slabs, bool grad, cudaStream_t s) {
   constexpr int NV = sizeof(T) == 4 ? 2 : 4;
-  // of a row of any phase that it may have
-  const int64_t units = (a.width + (AL ? 0 : 16 / (int)sizeof(T) - 1) + kUnit - 1) / kUnit;
-  if (units <= 32) return norm_launch<T, 1, 1, AL>(a, d, slab, slabs, grad, s);
-  if (NV == 4 && units <= 64) return norm_launch<T, 1, 2, AL>(a, d, slab, slabs, grad, s);
-  if (units <= 32 * NV) return norm_launch<T, 1, NV, AL>(a, d, slab, slabs, grad, s);
-  if (units <= 64 * NV) return norm_launch<T, 2, NV, AL>(a, d, slab, slabs, grad, s);
-  if (units <= 128 * NV) return norm_launch<T, 4, NV, AL>(a, d, slab, slabs, grad, s);
-  if (units <= 256 * NV) return norm_launch<T, 8, NV, AL>(a, d, slab, slabs, grad, s);
-  if (units <= 512 * NV) return norm_launch<T, 16, NV, AL>(a, d, slab, slabs, grad, s);
-  if constexpr (!AL && sizeof(T) == 4) {  // the widest rows, off the 16-byte grid: one unit more
-    if (units > 1024 * NV) return norm_launch<T, 32, 2 * NV, AL>(a, d, slab, slabs, grad, s);
+  const int units = (int)((a.width + (AL ? 0 : 16 / (int)sizeof(T) - 1) + kUnit - 1) / kUnit);
+  if (units <= 32) return norm_launch<T, true, 1, AL, false>(a, d, 1, slab, slabs, grad, s);
+  if (NV == 4 && units <= 64) return norm_launch<T, true, 2, AL, false>(a, d, 1, slab, slabs, grad, s);
+  if (units <= 32 * NV) return norm_launch<T, true, NV, AL, false>(a, d, 1, slab, slabs, grad, s);
+  const auto warps = [&](int nv) { return (units + 32 * nv - 1) / (32 * nv); };
+  if (NV == 4 && warps(3) <= 16 && warps(3) * 3 < warps(4) * 4) return norm_launch<T, false, NV == 4 ? 3 : NV, AL, false>(a, d, warps(3), slab, slabs, grad, s);
+  if (warps(NV) <= 16) return norm_launch<T, false, NV, AL, false>(a, d, warps(NV), slab, slabs, grad, s);
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (!AL)
+      if (warps(NV) > 32) return norm_launch<T, false, 2 * NV, AL, true>(a, d, warps(2 * NV), slab, slabs, grad, s);
+    return norm_launch<T, false, NV, AL, true>(a, d, warps(NV), slab, slabs, grad, s);
+  } else if constexpr (!AL) {
+    return norm_launch<T, false, NV, AL, true>(a, d, warps(NV), slab, slabs, grad, s);
   }
-  return norm_launch<T, 32, NV, AL>(a, d, slab, slabs, grad, s);
+  return cudaErrorInvalidValue;  // not reached: aligned bf16 rows of 16,384 columns take 16 warps
 }
 
 cudaError_t norm_any(const simx_norm& a, float* slab, int64_t& slabs, bool grad, cudaStream_t s) {
