@@ -101,7 +101,8 @@ struct Row {
   static __device__ __forceinline__ int phase(const T* p) { return (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T)); }
   __device__ __forceinline__ Raw<T> load(int v, int ph, int width) const {
     const int c0 = v * kUnit - ph;
-    if (AL || (on_grid && c0 + before >= 0 && c0 + kUnit <= after)) {
+    // inside the row, or at least inside the tensor
+    if (AL || (on_grid && ((c0 >= 0 && c0 + kUnit <= width) || (c0 + before >= 0 && c0 + kUnit <= after)))) {
       Raw<T> r;
       const uint4* g = reinterpret_cast<const uint4*>(p + c0);
 #pragma unroll
@@ -131,9 +132,19 @@ __device__ __forceinline__ int plane_of(int j, int ph, int pitch) {
   return ((j - ph) & 7) * pitch + (j < ph ? 0 : 1);
 }
 
-// The gains of unit v: from the caches, or from shared memory.
+// Where a thread finds its units' elements in such an array in a row of phase ph: element j of its unit k at
+// p[j][32 k].
+struct Places {
+  float* p[kUnit];
+  __device__ __forceinline__ Places(float* base, int v0, int ph, int pitch) {
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) p[j] = base + plane_of(j, ph, pitch) + v0;
+  }
+};
+
+// The gains of unit v, the thread's unit k: from the caches, or from shared memory.
 template <bool AL>
-__device__ __forceinline__ void gains(const float* gain, const float* sh, int v, int ph, int pitch, float (&w)[kUnit]) {
+__device__ __forceinline__ void gains(const float* gain, const Places& sh, int v, int k, float (&w)[kUnit]) {
   if (AL) {
     const float4 a = __ldg(reinterpret_cast<const float4*>(gain) + 2 * v), b = __ldg(reinterpret_cast<const float4*>(gain) + 2 * v + 1);
     const float q[kUnit] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -141,7 +152,7 @@ __device__ __forceinline__ void gains(const float* gain, const float* sh, int v,
     for (int j = 0; j < kUnit; ++j) w[j] = q[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) w[j] = sh[plane_of(j, ph, pitch) + v];
+    for (int j = 0; j < kUnit; ++j) w[j] = sh.p[j][32 * k];
   }
 }
 __device__ __forceinline__ void fill_gains(const float* gain, float* sh, int width) {
@@ -217,6 +228,7 @@ __global__ void __launch_bounds__((norm_threads<ONE, WIDE>()), (norm_blocks_per_
     const int ph = AL ? 0 : Row<T, AL>::phase(static_cast<const T*>(A.x) + i * A.x_ld);
     const int units = (ph + width + kUnit - 1) / kUnit;
     const Row<T, AL> x(A.x, i, A.x_ld, ph, A.n, width), res(A.residual, i, A.residual_ld, ph, A.n, width);
+    const Places gp(gs, first + lane, ph, pitch);
     Raw<T> rx[NV], rr[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -256,7 +268,7 @@ __global__ void __launch_bounds__((norm_threads<ONE, WIDE>()), (norm_blocks_per_
       const int v = first + 32 * k + lane;
       if (v >= units) continue;
       float w[kUnit], o[kUnit];
-      gains<AL>(A.gain, gs, v, ph, pitch, w);
+      gains<AL>(A.gain, gp, v, k, w);
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) o[j] = __fmul_rn(__fmul_rn(f[k][j], r), w[j]);
       if (A.z) z.store(v, ph, width, f[k]);
@@ -299,6 +311,7 @@ __global__ void __launch_bounds__((norm_threads<ONE, WIDE>()), (norm_blocks_per_
     const int ph = AL ? 0 : Row<T, AL>::phase(static_cast<const T*>(A.z) + i * A.z_ld);
     const int units = (ph + width + kUnit - 1) / kUnit;
     const Row<T, AL> z(A.z, i, A.z_ld, ph, A.n, width), dy(A.dy, i, A.dy_ld, ph, A.n, width), dz(A.dz, i, A.dz_ld, ph, A.n, width);
+    const Places gp(gs, first + lane, ph, pitch), sp(sums, lane, ph, SP);
     const float r = A.rstd[i];
     Raw<T> rz[NV], ry[NV], rd[NV];
 #pragma unroll
@@ -324,7 +337,7 @@ __global__ void __launch_bounds__((norm_threads<ONE, WIDE>()), (norm_blocks_per_
         ry[k] = masked(ry[k], c0, width);
       }
       float w[kUnit];
-      gains<AL>(A.gain, gs, v, ph, pitch, w);
+      gains<AL>(A.gain, gp, v, k, w);
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) {
         const float zh = __fmul_rn(elem(rz[k], j), r), d = elem(ry[k], j);
@@ -332,8 +345,7 @@ __global__ void __launch_bounds__((norm_threads<ONE, WIDE>()), (norm_blocks_per_
         if (AL) {
           acc[AL ? k : 0][j] = __fmaf_rn(d, zh, acc[AL ? k : 0][j]);
         } else if (slab) {
-          float* s = sums + plane_of(j, ph, SP) + 32 * k + lane;
-          *s = __fmaf_rn(d, zh, *s);
+          sp.p[j][32 * k] = __fmaf_rn(d, zh, sp.p[j][32 * k]);
         }
       }
     }
@@ -344,7 +356,7 @@ __global__ void __launch_bounds__((norm_threads<ONE, WIDE>()), (norm_blocks_per_
       const int v = first + 32 * k + lane;
       if (v >= units) continue;
       float w[kUnit], o[kUnit];
-      gains<AL>(A.gain, gs, v, ph, pitch, w);
+      gains<AL>(A.gain, gp, v, k, w);
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) {
         const float zh = __fmul_rn(elem(rz[k], j), r);
