@@ -109,21 +109,38 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// A sum as hi + lo, each addition's rounding error kept (Knuth's two-sum): about 46 bits.  fp64 runs at a
+// sixty-fourth of the fp32 rate here, and the few thousand additions of a call's statistics took longer in it than its rows.
+struct Sum2 {
+  float hi, lo;
+  __device__ __forceinline__ void add(float v, float rest) {
+    const float s = __fadd_rn(hi, v), b = __fsub_rn(s, hi);
+    const float e = __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(v, b));
+    hi = s;
+    lo = __fadd_rn(lo, __fadd_rn(e, rest));
+  }
+  // a sum that is not finite has no rounding error to give back
+  __device__ __forceinline__ float value() const { return fabsf(hi) < inf() ? __fadd_rn(hi, lo) : hi; }
+};
+
 // out[c] = the sum over the rows of part [rows][cols]: a block of 1024 threads for the 32 columns from c0
 // on, 32 rows at a time, joined in a fixed order.
 __device__ __forceinline__ void column_sums(const float* part, int64_t rows, int64_t cols, int64_t c0, float* out) {
   __shared__ float sh[32][33];
   const int cl = threadIdx.x & 31, rl = (int)threadIdx.x / 32;
   const int64_t c = c0 + cl;
-  float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  Sum2 t = {};
   if (c < cols) {
     int64_t r = rl;
-    for (; r + 96 < rows; r += 128)
+    for (; r + 96 < rows; r += 128) {
+      float v[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = __fadd_rn(v[u], part[(r + 32 * u) * cols + c]);
-    for (; r < rows; r += 32) v[0] = __fadd_rn(v[0], part[r * cols + c]);
+      for (int u = 0; u < 4; ++u) v[u] = part[(r + 32 * u) * cols + c];
+      t.add(__fadd_rn(__fadd_rn(v[0], v[1]), __fadd_rn(v[2], v[3])), 0.0f);
+    }
+    for (; r < rows; r += 32) t.add(part[r * cols + c], 0.0f);
   }
-  sh[rl][cl] = __fadd_rn(__fadd_rn(v[0], v[1]), __fadd_rn(v[2], v[3]));
+  sh[rl][cl] = t.value();
   __syncthreads();
   const float s = sum_lanes(sh[cl][rl]);
   if (cl == 0 && c0 + rl < cols) out[c0 + rl] = s;

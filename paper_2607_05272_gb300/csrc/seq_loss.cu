@@ -667,18 +667,6 @@ __global__ void __launch_bounds__(kClusterThreads, 1) k_token_cluster(TokenArgs 
   }
 }
 
-// A sum as hi + lo, each addition's rounding error kept (Knuth's two-sum): about 46 bits.  fp64 runs at a
-// sixty-fourth of the fp32 rate here, and these few thousand additions took longer in it than the rows.
-struct Sum2 {
-  float hi, lo;
-  __device__ __forceinline__ void add(float v, float rest) {
-    const float s = __fadd_rn(hi, v), b = __fsub_rn(s, hi);
-    const float e = __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(v, b));
-    hi = s;
-    lo = __fadd_rn(lo, __fadd_rn(e, rest));
-  }
-};
-
 // The statistics from the blocks' partial sums, in a fixed order.
 __global__ void __launch_bounds__(kStatThreads) k_token_stats(TokenArgs A, int parts) {
   __shared__ Sum2 sh[kStatThreads / 32][4];
@@ -699,20 +687,18 @@ __global__ void __launch_bounds__(kStatThreads) k_token_stats(TokenArgs A, int p
     for (int q = 0; q < 4; ++q) sh[threadIdx.x / 32][q] = v[q];
   __syncthreads();
   if (threadIdx.x >= 32) return;
-  float out = 0.0f;
   const int q = threadIdx.x & 3;
   Sum2 t = {};
   for (int w = 0; w < kStatThreads / 32; ++w) t.add(sh[w][q].hi, sh[w][q].lo);
-  out = __fadd_rn(t.hi, t.lo);
   // L = policy + c_kl kl - c_entropy entropy, from the two-part sums
   const float kh = __shfl_sync(0xffffffffu, t.hi, 1), kl = __shfl_sync(0xffffffffu, t.lo, 1);
   const float eh = __shfl_sync(0xffffffffu, t.hi, 2), el = __shfl_sync(0xffffffffu, t.lo, 2);
-  if (threadIdx.x < 4) A.stats[1 + q] = out;
+  if (threadIdx.x < 4) A.stats[1 + q] = t.value();
   if (threadIdx.x == 0) {
     const float a = __fmul_rn(A.c_kl, kh), b = __fmul_rn(-A.c_entropy, eh);
     t.add(a, __fmaf_rn(A.c_kl, kl, __fmaf_rn(A.c_kl, kh, -a)));
     t.add(b, __fmaf_rn(-A.c_entropy, el, __fmaf_rn(-A.c_entropy, eh, -b)));
-    A.stats[0] = __fadd_rn(t.hi, t.lo);
+    A.stats[0] = t.value();
   }
 }
 

@@ -459,9 +459,10 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
       }
     };
     bring(t0);
-    float bias[VEC], carry[VEC], db[VEC];
+    float bias[VEC], carry[VEC];
+    Sum2 db[VEC] = {};  // over all rounds: a long chain
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) bias[i] = carry[i] = db[i] = 0.0f;
+    for (int i = 0; i < VEC; ++i) bias[i] = carry[i] = 0.0f;
     if (mine) {
       load_bias<VEC>(A.bias, c, bias);
       load_row<VEC>(A.dh_last, b * A.channels + c, carry);
@@ -515,6 +516,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
       tile_states<VEC, DONE>(a, m, carry, mu, lcl, turn++, sh);
       T* px = dx;
       T* pg = dgate;
+      float round_db[VEC] = {};
 #pragma unroll
       for (int k = 0; k < S; ++k, px -= A.dx.st, pg -= A.dgate.st) {
         float ox[VEC], og[VEC];
@@ -523,7 +525,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
           const float lam = DONE && (own >> k & 1u) ? dt[k][i] : __fadd_rn(dt[k][i], mu[i]);
           ox[i] = __fmul_rn(bt[k][i], lam);
           og[i] = __fmul_rn(qt[k][i], lam);
-          db[i] = __fadd_rn(db[i], og[i]);  // steps that are not there: qt is 0
+          round_db[i] = __fadd_rn(round_db[i], og[i]);  // steps that are not there: qt is 0
           mu[i] = __fmaf_rn(-bt[k][i], lam, lam);
         }
         if (whole || (mine && t0 >= k)) {
@@ -531,6 +533,8 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
           store_vec(pg, og);
         }
       }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) db[i].add(round_db[i], 0.0f);
     }
     if (A.dh0 && mine && group == 0) {
 #pragma unroll
@@ -540,7 +544,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        float v = db[i];
+        float v = db[i].value();
         for (int d = 16 >> lcl; d > 0; d /= 2) v = __fadd_rn(v, __shfl_down_sync(0xffffffffu, v, d << lcl));
         if (lane < LC) reinterpret_cast<float*>(sh.table[0][warp][0])[cl * VEC + i] = v;
       }
@@ -812,7 +816,8 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
       if (DONE) next = u - cl >= 0 && cl <= S ? done_byte(A, b, u - cl) : (uint8_t)0;
     };
     bring(t0);
-    float bias[4] = {}, db[4] = {}, carry = joins && A.dh_last ? A.dh_last[b * A.channels + c0 + J.ch] : 0.0f;
+    Sum2 db[4] = {};  // over all rounds: a long chain
+    float bias[4] = {}, carry = joins && A.dh_last ? A.dh_last[b * A.channels + c0 + J.ch] : 0.0f;
     if (mine) load_bias<4>(A.bias, c, bias);
     for (int64_t round = 0; round < rounds; ++round, t0 -= step, dx -= step * A.dx.st, dgate -= step * A.dgate.st) {
       float bt[S][4], qt[S][4], dt[S][4], a[4], m[4], mu[4];  // 1 - a; a (1 - a) (s - x); dh
@@ -859,6 +864,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
       wide_states<NW, CLT, DONE>(a, m, carry, mu, rank, turn++, lost, sh);
       T* px = dx;
       T* pg = dgate;
+      float round_db[4] = {};
 #pragma unroll
       for (int k = 0; k < S; ++k, px -= A.dx.st, pg -= A.dgate.st) {
         float ox[4], og[4];
@@ -867,7 +873,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
           const float lam = DONE && (own >> k & 1u) ? dt[k][i] : __fadd_rn(dt[k][i], mu[i]);
           ox[i] = __fmul_rn(bt[k][i], lam);
           og[i] = __fmul_rn(qt[k][i], lam);
-          db[i] = __fadd_rn(db[i], og[i]);  // steps that are not there: qt is 0
+          round_db[i] = __fadd_rn(round_db[i], og[i]);  // steps that are not there: qt is 0
           mu[i] = __fmaf_rn(-bt[k][i], lam, lam);
         }
         if (whole || (mine && t0 >= k)) {
@@ -875,11 +881,13 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
           store_vec(pg, og);
         }
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) db[i].add(round_db[i], 0.0f);
     }
     if (A.dh0 && joins && rank == 0 && J.q == 0) A.dh0[b * A.channels + c0 + J.ch] = carry;
     if (part) {  // the block's sums of its steps, group by group
       __syncthreads();
-      sh.a[group * (kWidePitch / 4) + cl] = make_float4(db[0], db[1], db[2], db[3]);
+      sh.a[group * (kWidePitch / 4) + cl] = make_float4(db[0].value(), db[1].value(), db[2].value(), db[3].value());
       __syncthreads();
       if (threadIdx.x < kWideChannels && c0 + threadIdx.x < A.channels) {
         float v = 0.0f;
