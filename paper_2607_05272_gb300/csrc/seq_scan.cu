@@ -81,18 +81,16 @@ template <class T>
 __device__ __forceinline__ void store_vec(T* p, const float (&v)[1]) {
   *p = narrow<T>(v[0]);
 }
-// The same of fp32 rows (bias, states), which have no alignment of their own.
+// `count` channels of fp32 rows (states; bias log2 e), which have no alignment of their own.
 template <int VEC>
-__device__ __forceinline__ void load_row(const float* p, int64_t off, float (&v)[VEC]) {
+__device__ __forceinline__ void load_row(const float* p, int64_t off, float (&v)[VEC], int count = VEC) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) v[i] = p ? p[off + i] : 0.0f;
+  for (int i = 0; i < VEC; ++i) v[i] = p && i < count ? p[off + i] : 0.0f;
 }
-
-// bias log2 e
 template <int VEC>
-__device__ __forceinline__ void load_bias(const float* p, int64_t off, float (&v)[VEC]) {
+__device__ __forceinline__ void load_bias(const float* p, int64_t off, float (&v)[VEC], int count = VEC) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) v[i] = p ? __fmul_rn(p[off + i], kLog2e) : 0.0f;
+  for (int i = 0; i < VEC; ++i) v[i] = p && i < count ? __fmul_rn(p[off + i], kLog2e) : 0.0f;
 }
 
 // ---------------------------------------------------------------------------
@@ -561,7 +559,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
 }
 
 // ---------------------------------------------------------------------------
-// Wide tiles: 64 channels, 16 lanes of 4 each, in aligned tensors.
+// Wide tiles: 64 channels, 16 lanes of 4 each.
 // The same tile of steps in registers, with the joining done across the block instead of by every thread
 // for itself: the maps of all groups of lanes go to a table, where each thread takes 4 groups of one
 // channel (NW / 2 neighbouring lanes per channel), joins them, and writes back the state before each
@@ -571,6 +569,54 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
 // ---------------------------------------------------------------------------
 constexpr int kWideLanes = 16, kWideChannels = 64, kWidePitch = 68;
 constexpr int kMaxCluster = 8;
+
+// Steps of 4 channels of K tensors on their way in the thread's places in shared memory.  ALIGNED: one copy
+// of 4 elements a step; else element by element, of the `count` channels that there are: asynchronously
+// for fp32, by way of registers for bf16 (all of a tensor's steps on their way at once).
+template <class T, int K, int S, bool ALIGNED>
+struct WideAhead {
+  T* slot;
+  int pitch, count;
+  __device__ __forceinline__ void start(void* shared) {
+    slot = static_cast<T*>(shared) + (int)threadIdx.x * 4;
+    pitch = (int)blockDim.x * 4;
+  }
+  // Steps 0 .. steps - 1 at p, p + st, ...
+  __device__ __forceinline__ void bring(int k, const T* p, int64_t st, int steps = S) {
+    T* to = slot + k * S * pitch;
+    if (ALIGNED) {
+#pragma unroll
+      for (int s = 0; s < S; ++s, p += st)
+        if (s < steps) copy_async<4 * (int)sizeof(T)>(to + s * pitch, p);
+    } else if (sizeof(T) == 4) {
+#pragma unroll
+      for (int s = 0; s < S; ++s, p += st)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (s < steps && i < count) copy_async<4>(to + s * pitch + i, p + i);
+    } else {
+      T v[S][4];
+#pragma unroll
+      for (int s = 0; s < S; ++s, p += st)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[s][i] = s < steps && i < count ? p[i] : narrow<T>(0.0f);
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[s * pitch + i] = v[s][i];
+    }
+  }
+  __device__ __forceinline__ void take(int k, int s, float (&v)[4]) const { load_vec(slot + (k * S + s) * pitch, v); }
+  __device__ __forceinline__ void put(T* p, const float (&v)[4]) const {
+    if (ALIGNED) {
+      store_vec(p, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < count) p[i] = narrow<T>(v[i]);
+    }
+  }
+};
 
 template <int NW, int CLT>
 struct WideShared {
@@ -669,7 +715,7 @@ __device__ __forceinline__ uint32_t group_bits(uint8_t byte) {
   return __ballot_sync(0xffffffffu, byte != 0) >> ((int)threadIdx.x & 16) & 0xFFFFu;
 }
 
-template <class T, bool DONE, int CLT>
+template <class T, bool DONE, int CLT, bool ALIGNED>
 __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles) {
   constexpr int S = kTileSteps, NW = 8, TB = 2 * NW * S;
   constexpr int64_t step = (int64_t)CLT * TB;
@@ -681,13 +727,14 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
   wide_start(sh);
   const int64_t per = (A.channels + kWideChannels - 1) / kWideChannels;
   const int64_t rounds = (A.len + step - 1) / step;
-  Ahead<T, 4, 2, S> in;
+  WideAhead<T, 2, S, ALIGNED> in;
   in.start(slots);
   uint32_t turn = 0;
   bool lost = false;
   for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
     const int64_t b = tile / per, c0 = (tile - b * per) * kWideChannels, c = c0 + 4 * cl;
     const bool mine = c < A.channels, joins = c0 + J.ch < A.channels;
+    in.count = (int)(mine ? (A.channels - c < 4 ? A.channels - c : 4) : 0);
     int64_t t0 = (int64_t)rank * TB + group * S;
     const T* gate = at<const T>(A.gate, b, t0, c);  // of the round to come
     const T* x = at<const T>(A.x, b, t0, c);
@@ -695,14 +742,11 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
     uint8_t next = 0;                               // of the round to come: done at step t0 + cl - 1
     const auto bring = [&](int64_t u) {
       if (mine && u + S <= A.len) {
-        in.bring_all(0, gate, A.gate.st);
-        in.bring_all(1, x, A.x.st);
-      } else if (mine) {
-#pragma unroll 1
-        for (int k = 0; k < S && u + k < A.len; ++k) {
-          in.bring(0, k, gate + k * A.gate.st);
-          in.bring(1, k, x + k * A.x.st);
-        }
+        in.bring(0, gate, A.gate.st);
+        in.bring(1, x, A.x.st);
+      } else if (mine && u < A.len) {
+        in.bring(0, gate, A.gate.st, (int)(A.len - u));
+        in.bring(1, x, A.x.st, (int)(A.len - u));
       }
       copy_commit();
       gate += step * A.gate.st;
@@ -711,7 +755,7 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
     };
     bring(t0);
     float bias[4] = {}, carry = joins && A.h0 ? A.h0[b * A.channels + c0 + J.ch] : 0.0f;
-    if (mine) load_bias<4>(A.bias, c, bias);
+    if (mine) load_bias<4>(A.bias, c, bias, in.count);
     for (int64_t round = 0; round < rounds; ++round, t0 += step, h += step * A.h.st) {
       float bt[S][4], xt[S][4], a[4], s[4], st[4];
       const bool whole = mine && t0 + S <= A.len;
@@ -754,7 +798,7 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
           if (DONE && (resets >> k & 1u)) st[i] = 0.0f;
           st[i] = __fmaf_rn(bt[k][i], __fsub_rn(xt[k][i], st[i]), st[i]);
         }
-        if (whole || (mine && t0 + k < A.len)) store_vec(p, st);
+        if (whole || (mine && t0 + k < A.len)) in.put(p, st);
       }
     }
     if (CLT > 1 && A.h_last == A.h0) cluster_sync();  // h_last in place of h0, which every block has used by now
@@ -765,7 +809,7 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
 }
 
 // Backward, on the steps in reverse order; part [batch * CLT][channels]: sums of dgate (or null).
-template <class T, bool DONE, int CLT>
+template <class T, bool DONE, int CLT, bool ALIGNED>
 __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t tiles, float* part) {
   constexpr int S = kTileSteps, NW = 4, TB = 2 * NW * S;
   constexpr int64_t step = (int64_t)CLT * TB;
@@ -778,13 +822,14 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
   wide_start(sh);
   const int64_t per = (A.channels + kWideChannels - 1) / kWideChannels;
   const int64_t rounds = (A.len + step - 1) / step;
-  Ahead<T, 4, 4, S> in;
+  WideAhead<T, 4, S, ALIGNED> in;
   in.start(slots);
   uint32_t turn = 0;
   bool lost = false;
   for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
     const int64_t b = tile / per, c0 = (tile - b * per) * kWideChannels, c = c0 + 4 * cl;
     const bool mine = c < A.channels, joins = c0 + J.ch < A.channels;
+    in.count = (int)(mine ? (A.channels - c < 4 ? A.channels - c : 4) : 0);
     int64_t t0 = A.len - 1 - (int64_t)rank * TB - group * S;  // of the thread's first step of the walk
     const T* gate = at<const T>(A.gate, b, t0, c);            // of the round to come
     const T* x = at<const T>(A.x, b, t0, c);
@@ -795,18 +840,15 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
     uint8_t next = 0;                                         // of the round to come: done at step t0 - cl
     const auto bring = [&](int64_t u) {
       if (mine && u >= S) {
-        in.bring_all(0, gate, -A.gate.st);
-        in.bring_all(1, x, -A.x.st);
-        in.bring_all(2, dh, -A.dh.st);
-        in.bring_all(3, h, -A.h.st);
-      } else if (mine) {
-#pragma unroll 1
-        for (int k = 0; k < S && u - k >= 0; ++k) {
-          in.bring(0, k, gate - k * A.gate.st);
-          in.bring(1, k, x - k * A.x.st);
-          in.bring(2, k, dh - k * A.dh.st);
-          if (u - k > 0) in.bring(3, k, h - k * A.h.st);
-        }
+        in.bring(0, gate, -A.gate.st);
+        in.bring(1, x, -A.x.st);
+        in.bring(2, dh, -A.dh.st);
+        in.bring(3, h, -A.h.st);
+      } else if (mine && u >= 0) {
+        in.bring(0, gate, -A.gate.st, (int)u + 1);
+        in.bring(1, x, -A.x.st, (int)u + 1);
+        in.bring(2, dh, -A.dh.st, (int)u + 1);
+        in.bring(3, h, -A.h.st, (int)u);
       }
       copy_commit();
       gate -= step * A.gate.st;
@@ -818,7 +860,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
     bring(t0);
     Sum2 db[4] = {};  // over all rounds: a long chain
     float bias[4] = {}, carry = joins && A.dh_last ? A.dh_last[b * A.channels + c0 + J.ch] : 0.0f;
-    if (mine) load_bias<4>(A.bias, c, bias);
+    if (mine) load_bias<4>(A.bias, c, bias, in.count);
     for (int64_t round = 0; round < rounds; ++round, t0 -= step, dx -= step * A.dx.st, dgate -= step * A.dgate.st) {
       float bt[S][4], qt[S][4], dt[S][4], a[4], m[4], mu[4];  // 1 - a; a (1 - a) (s - x); dh
       const bool whole = mine && t0 >= S;
@@ -832,7 +874,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
         in.take(2, k, dt[k]);
         in.take(3, k, s);
         const bool fresh = DONE && (ends >> (k + 1) & 1u);
-        if (!whole && mine && t0 == k) load_row<4>(A.h0, b * A.channels + c, s);
+        if (!whole && mine && t0 == k) load_row<4>(A.h0, b * A.channels + c, s, in.count);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const Gate q = gate_of(__fmaf_rn(g[i], kLog2e, bias[i]));
@@ -877,8 +919,8 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
           mu[i] = __fmaf_rn(-bt[k][i], lam, lam);
         }
         if (whole || (mine && t0 >= k)) {
-          store_vec(px, ox);
-          store_vec(pg, og);
+          in.put(px, ox);
+          in.put(pg, og);
         }
       }
 #pragma unroll
@@ -905,39 +947,46 @@ __global__ void __launch_bounds__(1024) k_scan_dbias(const float* part, int64_t 
   column_sums(part, rows, channels, (int64_t)blockIdx.x * 32, dbias);
 }
 
-// How a call is cut.  columns: up to kColSteps steps.  Wide tiles: aligned tensors of more than 32
-// channels and at least half a block's steps, in clusters of so many blocks; else tiles of 1 << lcl lanes
-// per row of channels and `warps` warps.
+constexpr int kFwdWarps = 8, kFwdPerSm = 2, kGradWarps = 4, kGradPerSm = 3;
+
+// How a call is cut.  columns: up to kColSteps steps.  Else tiles of 1 << lcl lanes per row of channels and
+// `warps` warps, or wide tiles in clusters of so many blocks: whichever ends first, by the waves of blocks
+// over the GPU, the rounds that each block goes, and what a round takes (microseconds, measured over calls
+// of 9 to 1770 MB: tiles of aligned tensors 3.4 to 5, of others 0.8 to 1.3 with a quarter of the elements;
+// wide tiles 2.4 forward and 3.5 backward, off alignment 3.2 to 5.4 and 8.4 to 11, and a tenth more for a
+// cluster's posts).  So for one long bf16 sequence of 18 channels, 17 x 32,774 steps, clusters of 8 take 148
+// us and tiles 421, and for 115 x 6961 of 167 channels tiles 306 and clusters 436.
 struct ScanPlan {
   bool columns, wide;
   int lcl, warps, cluster;
   int64_t tiles;
 };
-ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, bool aligned, int max_warps, int per_sm) {
+ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, bool aligned, bool grad) {
   ScanPlan p{};
   p.columns = len <= kColSteps;
-  p.cluster = 1;
-  const int vec = aligned ? 4 : 1;
-  const int64_t block = (int64_t)max_warps * 2 * kTileSteps;  // a wide block's steps
-  p.wide = !p.columns && aligned && channels > 32 && 2 * len >= block;
+  p.cluster = p.warps = 1;
+  if (p.columns) return p;
+  const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  const int max_warps = grad ? kGradWarps : kFwdWarps, vec = aligned ? 4 : 1;
+  const int64_t slots = (int64_t)sm_count() * (grad ? kGradPerSm : kFwdPerSm);
   while (p.lcl < (aligned ? 4 : 5) && ((int64_t)vec << p.lcl) < channels) ++p.lcl;
-  const int64_t width = p.wide ? kWideChannels : (int64_t)vec << p.lcl;
-  p.tiles = batch * ((channels + width - 1) / width);
-  p.warps = 1;
-  while (p.warps < max_warps && p.warps * (int64_t)(32 >> p.lcl) * kTileSteps < len) p.warps *= 2;
-  if (p.wide) {
-    // The cluster that ends first: waves of blocks over the GPU, each 1 / cluster of the steps, and a tenth
-    // more for the posts.
-    const int64_t slots = (int64_t)sm_count() * per_sm;
-    double best = 0.0;
-    for (int cl = 1; cl <= kMaxCluster && (cl == 1 || block * cl <= len); cl *= 2) {
-      const double cost = (double)((p.tiles * cl + slots - 1) / slots) / cl * (cl > 1 ? 1.1 : 1.0);
-      if (cl == 1 || cost < best * 0.99) {
-        best = cost;
-        p.cluster = cl;
-      }
+  p.tiles = batch * up(channels, (int64_t)vec << p.lcl);
+  const int64_t warp_steps = (int64_t)(32 >> p.lcl) * kTileSteps;
+  while (p.warps < max_warps && p.warps * warp_steps < len) p.warps *= 2;
+  double best = (double)up(p.tiles, slots * max_warps / p.warps) * (double)up(len, p.warps * warp_steps) * (aligned ? 3.6 : 0.95);
+  const int64_t block = (int64_t)max_warps * 2 * kTileSteps;  // a wide block's steps
+  const int64_t tiles = batch * up(channels, kWideChannels);
+  const double round = aligned ? (grad ? 3.5 : 2.5) : (grad ? 10.0 : 5.0);
+  // off alignment only large clusters are ever the better choice
+  for (int cl = aligned ? 1 : 4; cl <= kMaxCluster && (cl == 1 || block * cl <= len); cl *= 2) {
+    const double cost = (double)up(tiles * cl, slots) * (double)up(len, block * cl) * round * (cl > 1 ? 1.1 : 1.0);
+    if (cost < best) {
+      best = cost;
+      p.wide = true;
+      p.cluster = cl;
     }
   }
+  if (p.wide) p.tiles = tiles;
   return p;
 }
 
@@ -969,41 +1018,41 @@ cudaError_t launch_tiles(K* kernel, const ScanPlan& p, int threads, size_t smem,
   return cudaLaunchKernelEx(&lc, kernel, args...);
 }
 
-constexpr int kFwdWarps = 8, kFwdPerSm = 2, kGradWarps = 4, kGradPerSm = 3;
-
-template <class T, bool DONE>
-cudaError_t scan_tiles(const simx_scan& a, const ScanPlan& p, bool v4, cudaStream_t s) {
+template <class T, bool DONE, bool ALIGNED>
+cudaError_t scan_tiles(const simx_scan& a, const ScanPlan& p, cudaStream_t s) {
   if (p.wide) {
     const int th = 32 * kFwdWarps;
     const size_t smem = (size_t)th * 2 * kTileSteps * 4 * sizeof(T);
-    if (p.cluster == 8) return launch_tiles(k_scan_wide<T, DONE, 8>, p, th, smem, s, a, p.tiles);
-    if (p.cluster == 4) return launch_tiles(k_scan_wide<T, DONE, 4>, p, th, smem, s, a, p.tiles);
-    if (p.cluster == 2) return launch_tiles(k_scan_wide<T, DONE, 2>, p, th, smem, s, a, p.tiles);
-    return launch_tiles(k_scan_wide<T, DONE, 1>, p, th, smem, s, a, p.tiles);
+    if (p.cluster == 8) return launch_tiles(k_scan_wide<T, DONE, 8, ALIGNED>, p, th, smem, s, a, p.tiles);
+    if (p.cluster == 4) return launch_tiles(k_scan_wide<T, DONE, 4, ALIGNED>, p, th, smem, s, a, p.tiles);
+    if constexpr (ALIGNED) {
+      if (p.cluster == 2) return launch_tiles(k_scan_wide<T, DONE, 2, true>, p, th, smem, s, a, p.tiles);
+      return launch_tiles(k_scan_wide<T, DONE, 1, true>, p, th, smem, s, a, p.tiles);
+    }
   }
-  const size_t smem = (size_t)p.warps * 32 * 2 * kTileSteps * 4 * sizeof(T);
-  if (v4) return launch_tiles(k_scan_tiles<T, 4, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles);
-  return launch_tiles(k_scan_tiles<T, 1, DONE>, p, 32 * p.warps, 0, s, a, p.lcl, p.tiles);
+  const size_t smem = ALIGNED ? (size_t)p.warps * 32 * 2 * kTileSteps * 4 * sizeof(T) : 0;
+  return launch_tiles(k_scan_tiles<T, ALIGNED ? 4 : 1, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles);
 }
-template <class T, bool DONE>
-cudaError_t scan_grad_tiles(const simx_scan& a, const ScanPlan& p, bool v4, float* part, cudaStream_t s) {
+template <class T, bool DONE, bool ALIGNED>
+cudaError_t scan_grad_tiles(const simx_scan& a, const ScanPlan& p, float* part, cudaStream_t s) {
   if (p.wide) {
     const int th = 32 * kGradWarps;
     const size_t smem = (size_t)th * 4 * kTileSteps * 4 * sizeof(T);
-    if (p.cluster == 8) return launch_tiles(k_scan_grad_wide<T, DONE, 8>, p, th, smem, s, a, p.tiles, part);
-    if (p.cluster == 4) return launch_tiles(k_scan_grad_wide<T, DONE, 4>, p, th, smem, s, a, p.tiles, part);
-    if (p.cluster == 2) return launch_tiles(k_scan_grad_wide<T, DONE, 2>, p, th, smem, s, a, p.tiles, part);
-    return launch_tiles(k_scan_grad_wide<T, DONE, 1>, p, th, smem, s, a, p.tiles, part);
+    if (p.cluster == 8) return launch_tiles(k_scan_grad_wide<T, DONE, 8, ALIGNED>, p, th, smem, s, a, p.tiles, part);
+    if (p.cluster == 4) return launch_tiles(k_scan_grad_wide<T, DONE, 4, ALIGNED>, p, th, smem, s, a, p.tiles, part);
+    if constexpr (ALIGNED) {
+      if (p.cluster == 2) return launch_tiles(k_scan_grad_wide<T, DONE, 2, true>, p, th, smem, s, a, p.tiles, part);
+      return launch_tiles(k_scan_grad_wide<T, DONE, 1, true>, p, th, smem, s, a, p.tiles, part);
+    }
   }
-  const size_t smem = (size_t)p.warps * 32 * 4 * kTileSteps * 4 * sizeof(T);
-  if (v4) return launch_tiles(k_scan_grad_tiles<T, 4, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles, part);
-  return launch_tiles(k_scan_grad_tiles<T, 1, DONE>, p, 32 * p.warps, 0, s, a, p.lcl, p.tiles, part);
+  const size_t smem = ALIGNED ? (size_t)p.warps * 32 * 4 * kTileSteps * 4 * sizeof(T) : 0;
+  return launch_tiles(k_scan_grad_tiles<T, ALIGNED ? 4 : 1, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles, part);
 }
 
 template <class T>
 cudaError_t scan(const simx_scan& a, cudaStream_t s) {
   const bool v4 = a.channels % 4 == 0 && (a.len == 0 || (vectors<T>(a, a.x) && vectors<T>(a, a.gate) && vectors<T>(a, a.h)));
-  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4, kFwdWarps, kFwdPerSm);
+  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4, false);
   if (p.columns) {
     const int64_t cols = a.batch * (v4 ? a.channels / 4 : a.channels);
     const unsigned blocks = (unsigned)((cols + kColThreads - 1) / kColThreads);
@@ -1012,14 +1061,15 @@ cudaError_t scan(const simx_scan& a, cudaStream_t s) {
     count_launches(1);
     return cudaGetLastError();
   }
-  return a.done ? scan_tiles<T, true>(a, p, v4, s) : scan_tiles<T, false>(a, p, v4, s);
+  if (v4) return a.done ? scan_tiles<T, true, true>(a, p, s) : scan_tiles<T, false, true>(a, p, s);
+  return a.done ? scan_tiles<T, true, false>(a, p, s) : scan_tiles<T, false, false>(a, p, s);
 }
 
 template <class T>
 cudaError_t scan_grad(const simx_scan& a, float* part, int64_t& rows, cudaStream_t s) {
   const bool v4 = a.channels % 4 == 0 && (a.len == 0 || (vectors<T>(a, a.x) && vectors<T>(a, a.gate) && vectors<T>(a, a.h) &&
                                                          vectors<T>(a, a.dh) && vectors<T>(a, a.dx) && vectors<T>(a, a.dgate)));
-  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4, kGradWarps, kGradPerSm);
+  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4, true);
   rows = a.batch * p.cluster;
   if (p.columns) {
     const int64_t cols = a.batch * (v4 ? a.channels / 4 : a.channels);
@@ -1029,16 +1079,18 @@ cudaError_t scan_grad(const simx_scan& a, float* part, int64_t& rows, cudaStream
     count_launches(1);
     return cudaGetLastError();
   }
-  return a.done ? scan_grad_tiles<T, true>(a, p, v4, part, s) : scan_grad_tiles<T, false>(a, p, v4, part, s);
+  if (v4) return a.done ? scan_grad_tiles<T, true, true>(a, p, part, s) : scan_grad_tiles<T, false, true>(a, p, part, s);
+  return a.done ? scan_grad_tiles<T, true, false>(a, p, part, s) : scan_grad_tiles<T, false, false>(a, p, part, s);
 }
 
 }  // namespace
 
-// The backward pass's sums of dgate: a row of channels per batch entry and block of a cluster (the plan of
-// aligned tensors, whose clusters may be larger than one).
+// The backward pass's sums of dgate: a row of channels per batch entry and block of a cluster, of whichever
+// plan the tensors' alignment gives.
 size_t scan_workspace_bytes(int64_t batch, int64_t len, int64_t channels) {
-  const ScanPlan p = plan_scan(batch, len, channels, true, kGradWarps, kGradPerSm);
-  return (size_t)batch * (size_t)p.cluster * (size_t)channels * sizeof(float);
+  const int cl = std::max(plan_scan(batch, len, channels, true, true).cluster,
+                          plan_scan(batch, len, channels, false, true).cluster);
+  return (size_t)batch * (size_t)cl * (size_t)channels * sizeof(float);
 }
 
 cudaError_t launch_scan(const simx_scan& a, cudaStream_t s) {
