@@ -458,7 +458,8 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
     };
     bring(t0);
     float bias[VEC], carry[VEC];
-    Sum2 db[VEC] = {};  // over all rounds: a long chain
+    Sum2 db[VEC] = {};        // of dgate over all rounds, a long chain,
+    float db16[VEC] = {};     // and over up to 16 of them
 #pragma unroll
     for (int i = 0; i < VEC; ++i) bias[i] = carry[i] = 0.0f;
     if (mine) {
@@ -514,7 +515,6 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
       tile_states<VEC, DONE>(a, m, carry, mu, lcl, turn++, sh);
       T* px = dx;
       T* pg = dgate;
-      float round_db[VEC] = {};
 #pragma unroll
       for (int k = 0; k < S; ++k, px -= A.dx.st, pg -= A.dgate.st) {
         float ox[VEC], og[VEC];
@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
           const float lam = DONE && (own >> k & 1u) ? dt[k][i] : __fadd_rn(dt[k][i], mu[i]);
           ox[i] = __fmul_rn(bt[k][i], lam);
           og[i] = __fmul_rn(qt[k][i], lam);
-          round_db[i] = __fadd_rn(round_db[i], og[i]);  // steps that are not there: qt is 0
+          db16[i] = __fadd_rn(db16[i], og[i]);  // steps that are not there: qt is 0
           mu[i] = __fmaf_rn(-bt[k][i], lam, lam);
         }
         if (whole || (mine && t0 >= k)) {
@@ -531,8 +531,13 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
           store_vec(pg, og);
         }
       }
+      if ((round & 15) == 15 || round + 1 == rounds) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) db[i].add(round_db[i], 0.0f);
+        for (int i = 0; i < VEC; ++i) {
+          db[i].add(db16[i], 0.0f);
+          db16[i] = 0.0f;
+        }
+      }
     }
     if (A.dh0 && mine && group == 0) {
 #pragma unroll
@@ -858,7 +863,8 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
       if (DONE) next = u - cl >= 0 && cl <= S ? done_byte(A, b, u - cl) : (uint8_t)0;
     };
     bring(t0);
-    Sum2 db[4] = {};  // over all rounds: a long chain
+    Sum2 db[4] = {};     // of dgate over all rounds, a long chain,
+    float db16[4] = {};  // and over up to 16 of them
     float bias[4] = {}, carry = joins && A.dh_last ? A.dh_last[b * A.channels + c0 + J.ch] : 0.0f;
     if (mine) load_bias<4>(A.bias, c, bias, in.count);
     for (int64_t round = 0; round < rounds; ++round, t0 -= step, dx -= step * A.dx.st, dgate -= step * A.dgate.st) {
@@ -906,7 +912,6 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
       wide_states<NW, CLT, DONE>(a, m, carry, mu, rank, turn++, lost, sh);
       T* px = dx;
       T* pg = dgate;
-      float round_db[4] = {};
 #pragma unroll
       for (int k = 0; k < S; ++k, px -= A.dx.st, pg -= A.dgate.st) {
         float ox[4], og[4];
@@ -915,7 +920,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
           const float lam = DONE && (own >> k & 1u) ? dt[k][i] : __fadd_rn(dt[k][i], mu[i]);
           ox[i] = __fmul_rn(bt[k][i], lam);
           og[i] = __fmul_rn(qt[k][i], lam);
-          round_db[i] = __fadd_rn(round_db[i], og[i]);  // steps that are not there: qt is 0
+          db16[i] = __fadd_rn(db16[i], og[i]);  // steps that are not there: qt is 0
           mu[i] = __fmaf_rn(-bt[k][i], lam, lam);
         }
         if (whole || (mine && t0 >= k)) {
@@ -923,8 +928,13 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
           in.put(pg, og);
         }
       }
+      if ((round & 15) == 15 || round + 1 == rounds) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) db[i].add(round_db[i], 0.0f);
+        for (int i = 0; i < 4; ++i) {
+          db[i].add(db16[i], 0.0f);
+          db16[i] = 0.0f;
+        }
+      }
     }
     if (A.dh0 && joins && rank == 0 && J.q == 0) A.dh0[b * A.channels + c0 + J.ch] = carry;
     if (part) {  // the block's sums of its steps, group by group
