@@ -180,6 +180,8 @@ SIGNATURES = [
 def lib():
     """Load libsimx.so (built by build.py); raise if it is missing."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -535,63 +537,65 @@ def _refuse(msg: str):
     raise SimxError(EINVAL, msg)
 
 
-def _tensor(t, name: str, like):
-    """A data tensor: `like`'s dtype, shape and device, unit stride along the last axis."""
+def _tensor(t, name: str, like, shape, dev: int):
+    """A data tensor: `like`'s dtype, `shape`, on device `dev`, unit stride along the last axis."""
     if t is None:
         return None
-    if t.dtype is not like.dtype or t.shape != like.shape or t.device != like.device:
+    if t.dtype is not like.dtype or t.shape != shape or t.get_device() != dev:
         _refuse("%s: %s %s on %s expected, got %s %s on %s" % (
-            name, tuple(like.shape), like.dtype, like.device, tuple(t.shape), t.dtype, t.device))
-    if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():
+            name, tuple(shape), like.dtype, like.device, tuple(t.shape), t.dtype, t.device))
+    if not t.is_contiguous() and t.stride(-1) != 1 and t.shape[-1] > 1:
         _refuse("%s: the last axis needs unit stride" % name)
     return t.data_ptr()
 
 
-def _flat(t, name: str, dtype, shape, device):
-    """A contiguous tensor of `dtype` and `shape` on `device`."""
+def _flat(t, name: str, dtype, shape, dev: int):
+    """A contiguous tensor of `dtype` and `shape` on device `dev`."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        _refuse("%s: contiguous %s %s on %s expected, got %s %s on %s" % (
-            name, tuple(shape), dtype, device, tuple(t.shape), t.dtype, t.device))
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse("%s: contiguous %s %s on cuda:%d expected, got %s %s on %s" % (
+            name, tuple(shape), dtype, dev, tuple(t.shape), t.dtype, t.device))
     return t.data_ptr()
 
 
 def _dtype(t, name: str, ndim: int):
-    """(torch, dtype code, device) of an operator's leading tensor."""
+    """(torch, dtype code, shape, device index) of an operator's leading tensor."""
     import torch
     if not isinstance(t, torch.Tensor) or t.dim() != ndim:
         _refuse("%s: a tensor of %d axes expected" % (name, ndim))
     if not t.is_cuda:
         _refuse("%s: not on a CUDA device" % name)
-    if t.get_device() != torch.cuda.current_device():
+    dev = t.get_device()
+    if dev != torch.cuda.current_device():
         _refuse("%s: on %s, which is not the current device" % (name, t.device))
     if t.dtype is torch.float32:
-        return torch, 0, t.device
+        return torch, 0, t.shape, dev
     if t.dtype is torch.bfloat16:
-        return torch, 1, t.device
+        return torch, 1, t.shape, dev
     _refuse("%s: float32 or bfloat16 expected, got %s" % (name, t.dtype))
 
 
-def _workspace(ws, device):
+def _workspace(ws, dev: int):
     """(pointer, bytes) of a workspace tensor or None."""
     if ws is None:
         return None, 0
-    if ws.device != device or not ws.is_contiguous():
-        _refuse("workspace: a contiguous tensor on %s expected" % device)
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    if ws.get_device() != dev or not ws.is_contiguous():
+        _refuse("workspace: a contiguous tensor on cuda:%d expected" % dev)
+    return ws.data_ptr(), ws.nbytes
 
 
-def _ld(t) -> int:
+def _ld(t, shape) -> int:
     """Row stride of a [n, width] tensor (a single row has none)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.stride(0) if shape[0] > 1 else shape[1]
 
 
 def _logits(logits, grad, temperature):
-    torch, dt, dev = _dtype(logits, "logits", 2)
-    n, vocab = logits.shape
-    return torch, dev, n, Logits(_tensor(logits, "logits", logits), _tensor(grad, "grad", logits),
-                                 _ld(logits), _ld(grad) if grad is not None else 0, n, vocab, dt,
+    torch, dt, shape, dev = _dtype(logits, "logits", 2)
+    n, vocab = shape
+    return torch, dev, n, Logits(_tensor(logits, "logits", logits, shape, dev),
+                                 _tensor(grad, "grad", logits, shape, dev), _ld(logits, shape),
+                                 _ld(grad, shape) if grad is not None else 0, n, vocab, dt,
                                  temperature)
 
 
@@ -650,25 +654,29 @@ def gated_scan_workspace_size(batch: int, length: int, channels: int) -> int:
     return lib().simx_gated_scan_workspace_size(batch, length, channels)
 
 
-def _seq(t, name: str, like):
-    """A Seq of a tensor of `like`'s shape."""
-    p = _tensor(t, name, like)
-    return Seq(p, t.stride(0), t.stride(1)) if t is not None else Seq()
+def _seq(t, name: str, like, shape, dev: int):
+    """A Seq of a tensor of `like`'s dtype."""
+    p = _tensor(t, name, like, shape, dev)
+    if t is None:
+        return Seq()
+    sb, st, _ = t.stride()
+    return Seq(p, sb, st)
 
 
 def _scan(x, gate, h, bias, h0, done):
-    torch, dt, dev = _dtype(x, "x", 3)
-    b, t, c = x.shape
+    torch, dt, shape, dev = _dtype(x, "x", 3)
+    b, t, c = shape
     d, dsb, dst = None, 0, 0
     if done is not None:
-        if done.dtype is not torch.uint8 or done.shape != (b, t) or done.device != dev:
-            _refuse("done: uint8 %s on %s expected" % ((b, t), dev))
+        if done.dtype is not torch.uint8 or done.shape != (b, t) or done.get_device() != dev:
+            _refuse("done: uint8 %s on cuda:%d expected" % ((b, t), dev))
         d = done.data_ptr()
         dsb, dst = done.stride()
     f = torch.float32
-    return f, (b, c), dev, Scan(b, t, c, dt, _seq(x, "x", x), _seq(gate, "gate", x), _seq(h, "h", x),
-                                _flat(bias, "bias", f, (c,), dev), _flat(h0, "h0", f, (b, c), dev),
-                                d, dsb, dst)
+    return f, shape, dev, Scan(b, t, c, dt, _seq(x, "x", x, shape, dev),
+                               _seq(gate, "gate", x, shape, dev), _seq(h, "h", x, shape, dev),
+                               _flat(bias, "bias", f, (c,), dev),
+                               _flat(h0, "h0", f, (b, c), dev), d, dsb, dst)
 
 
 def gated_scan(x, gate, h, workspace=None, bias=None, h0=None, done=None, h_last=None, stream=None):
@@ -676,8 +684,8 @@ def gated_scan(x, gate, h, workspace=None, bias=None, h0=None, done=None, h_last
     [batch, len, channels] of any batch and time strides (simx_gated_scan).  bias: fp32 [channels];
     h0, h_last: fp32 [batch, channels] (h_last may be h0: the single-token step of serving); done:
     uint8 [batch, len], nonzero where the state is not carried on; each of them may be None."""
-    f, state, dev, s = _scan(x, gate, h, bias, h0, done)
-    s.h_last = _flat(h_last, "h_last", f, state, dev)
+    f, (b, _, c), dev, s = _scan(x, gate, h, bias, h0, done)
+    s.h_last = _flat(h_last, "h_last", f, (b, c), dev)
     _check(lib().simx_gated_scan(C.byref(s), *_workspace(workspace, dev), _stream(stream)))
 
 
@@ -685,27 +693,29 @@ def gated_scan_grad(x, gate, h, dh, dx, dgate, workspace, bias=None, h0=None, do
                     dh_last=None, dbias=None, dh0=None, stream=None):
     """The backward pass of gated_scan (simx_gated_scan_grad): dx, dgate and, where given, dbias
     and dh0 from dh and dh_last, with h as the forward pass left it."""
-    f, state, dev, s = _scan(x, gate, h, bias, h0, done)
-    s.dh, s.dx, s.dgate = _seq(dh, "dh", x), _seq(dx, "dx", x), _seq(dgate, "dgate", x)
+    f, shape, dev, s = _scan(x, gate, h, bias, h0, done)
+    state = (shape[0], shape[2])
+    s.dh, s.dx = _seq(dh, "dh", x, shape, dev), _seq(dx, "dx", x, shape, dev)
+    s.dgate = _seq(dgate, "dgate", x, shape, dev)
     s.dh_last = _flat(dh_last, "dh_last", f, state, dev)
     s.dbias = _flat(dbias, "dbias", f, state[1:], dev)
     s.dh0 = _flat(dh0, "dh0", f, state, dev)
     _check(lib().simx_gated_scan_grad(C.byref(s), *_workspace(workspace, dev), _stream(stream)))
 
 
-def _rows(t, name: str, like):
-    """(pointer, row stride) of a tensor of `like`'s shape."""
-    return (_tensor(t, name, like), _ld(t)) if t is not None else (None, 0)
+def _rows(t, name: str, like, shape, dev: int):
+    """(pointer, row stride) of a tensor of `like`'s dtype."""
+    return (_tensor(t, name, like, shape, dev), _ld(t, shape)) if t is not None else (None, 0)
 
 
 def _norm(like, name: str, gain, rstd, p, eps, seed, step, row_base):
-    torch, dt, dev = _dtype(like, name, 2)
-    n, width = like.shape
+    torch, dt, shape, dev = _dtype(like, name, 2)
+    n, width = shape
     if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 32 and 0 <= row_base < 1 << 32):
         _refuse("seed, step or row_base out of range")
     f = torch.float32
-    return f, dev, (n, width, dt, p, eps, seed, step, row_base, _flat(gain, "gain", f, (width,), dev),
-                    _flat(rstd, "rstd", f, (n,), dev))
+    return f, shape, dev, (n, width, dt, p, eps, seed, step, row_base,
+                           _flat(gain, "gain", f, (width,), dev), _flat(rstd, "rstd", f, (n,), dev))
 
 
 def dropout_add_norm(x, gain, y, residual=None, z=None, rstd=None, p: float = 0.0,
@@ -714,9 +724,9 @@ def dropout_add_norm(x, gain, y, residual=None, z=None, rstd=None, p: float = 0.
     """z = residual + dropout_p(x) and y = rms_norm(z) * gain over rows [n, width]
     (simx_dropout_add_norm).  The mask is a function of (seed, step, row_base + row, column) and is
     not stored.  gain: fp32 [width]; rstd: fp32 [n] or None, kept for the backward pass."""
-    _, _, head = _norm(x, "x", gain, rstd, p, eps, seed, step, row_base)
-    a = Norm(*head, *_rows(x, "x", x), *_rows(residual, "residual", x), *_rows(z, "z", x),
-             *_rows(y, "y", x))
+    _, n, dev, head = _norm(x, "x", gain, rstd, p, eps, seed, step, row_base)
+    a = Norm(*head, *_rows(x, "x", x, n, dev), *_rows(residual, "residual", x, n, dev),
+             *_rows(z, "z", x, n, dev), *_rows(y, "y", x, n, dev))
     _check(lib().simx_dropout_add_norm(C.byref(a), _stream(stream)))
 
 
@@ -730,10 +740,10 @@ def dropout_add_norm_grad(z, gain, rstd, dy, dx, workspace, dz=None, dresidual=N
     """The backward pass of dropout_add_norm (simx_dropout_add_norm_grad): dx, dresidual and dgain
     (each may be None) from dy and dz, with z and rstd as the forward pass left them and the same
     p, seed, step and row_base."""
-    f, dev, head = _norm(z, "z", gain, rstd, p, 0.0, seed, step, row_base)
-    a = Norm(*head, None, 0, None, 0, *_rows(z, "z", z), None, 0, *_rows(dy, "dy", z),
-             *_rows(dz, "dz", z), *_rows(dx, "dx", z), *_rows(dresidual, "dresidual", z),
-             _flat(dgain, "dgain", f, z.shape[1:], dev))
+    f, n, dev, head = _norm(z, "z", gain, rstd, p, 0.0, seed, step, row_base)
+    a = Norm(*head, None, 0, None, 0, *_rows(z, "z", z, n, dev), None, 0,
+             *_rows(dy, "dy", z, n, dev), *_rows(dz, "dz", z, n, dev), *_rows(dx, "dx", z, n, dev),
+             *_rows(dresidual, "dresidual", z, n, dev), _flat(dgain, "dgain", f, n[1:], dev))
     _check(lib().simx_dropout_add_norm_grad(C.byref(a), *_workspace(workspace, dev), _stream(stream)))
 
 
