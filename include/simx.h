@@ -597,7 +597,7 @@ typedef struct simx_scan {
   float* dbias;
   float* dh0;
 } simx_scan;
-/* Covers both passes; it is 0 where neither needs one (the workspace may then be NULL). */
+/* Of the backward pass; the forward pass uses none (its workspace may be NULL). */
 size_t simx_gated_scan_workspace_size(int64_t batch, int64_t len, int64_t channels);
 simx_status simx_gated_scan(const simx_scan* s, void* d_workspace, size_t workspace_bytes, void* stream);
 simx_status simx_gated_scan_grad(const simx_scan* s, void* d_workspace, size_t workspace_bytes,

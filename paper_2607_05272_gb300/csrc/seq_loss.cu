@@ -861,7 +861,7 @@ cudaError_t token_cluster(const TokenArgs& a, int& parts, cudaStream_t s) {
 
 template <class T, int NT>
 cudaError_t token_stream(const TokenArgs& a, int& parts, cudaStream_t s) {
-  parts = (int)std::min<int64_t>(std::min<int64_t>(a.n, (int64_t)sm_count() * (1024 / NT)), kMaxParts);
+  parts = (int)std::min<int64_t>(a.n, kMaxParts);  // a row or few per block: those without weight leave room for others
   if (a.c_entropy != 0.0f && a.g) k_token_stream<T, NT, true><<<parts, NT, 0, s>>>(a);
   else k_token_stream<T, NT, false><<<parts, NT, 0, s>>>(a);
   count_launches(1);
@@ -949,8 +949,8 @@ cudaError_t pref_rows(const PrefArgs& a, bool grad, cudaStream_t s) {
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
-  const int64_t most = (int64_t)sm_count() * (1024 / NT);
-  lc.gridDim = dim3((unsigned)std::max<int64_t>(1, grad && !a.g ? 1 : std::min(a.n, grad ? 2 * most : most)));
+  // a block per row up to a million rows: those that are masked leave room for others
+  lc.gridDim = dim3((unsigned)std::max<int64_t>(1, grad && !a.g ? 1 : std::min<int64_t>(a.n, 1 << 20)));
   lc.blockDim = dim3(NT);
   lc.stream = s;
   lc.attrs = at;
