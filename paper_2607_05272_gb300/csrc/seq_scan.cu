@@ -961,11 +961,12 @@ constexpr int kFwdWarps = 8, kFwdPerSm = 2, kGradWarps = 4, kGradPerSm = 3;
 
 // How a call is cut.  columns: up to kColSteps steps.  Else tiles of 1 << lcl lanes per row of channels and
 // `warps` warps, or wide tiles in clusters of so many blocks: whichever ends first, by the waves of blocks
-// over the GPU, the rounds that each block goes, and what a round takes (microseconds, measured over calls
-// of 9 to 1770 MB: tiles of aligned tensors 3.4 to 5, of others 0.8 to 1.3 with a quarter of the elements;
-// wide tiles 2.4 forward and 3.5 backward, off alignment 3.2 to 5.4 and 8.4 to 11, and a tenth more for a
-// cluster's posts).  So for one long bf16 sequence of 18 channels, 17 x 32,774 steps, clusters of 8 take 148
-// us and tiles 421, and for 115 x 6961 of 167 channels tiles 306 and clusters 436.
+// over the GPU, the rounds that each block goes (and one for its first loads), and what a round takes
+// (microseconds, measured over calls of 9 to 1770 MB: tiles of aligned tensors 3.4 to 5, of others 0.8 to
+// 1.3 with a quarter of the elements; wide tiles 2.4 forward and 3.5 backward, off alignment 3.2 to 5.4 and
+// 8.4 to 11, and up to a quarter more for a cluster's posts).  One long bf16 sequence of 18 channels, 17 x
+// 32,774 steps: clusters of 8 148 us, tiles 421; 115 x 6961 of 167 channels: tiles 306, clusters 436;
+// backward 16 x 2048 x 2048: clusters of 1, 2, 4, 8 201, 169, 167, 193.
 struct ScanPlan {
   bool columns, wide;
   int lcl, warps, cluster;
@@ -983,13 +984,14 @@ ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, bool aligned, b
   p.tiles = batch * up(channels, (int64_t)vec << p.lcl);
   const int64_t warp_steps = (int64_t)(32 >> p.lcl) * kTileSteps;
   while (p.warps < max_warps && p.warps * warp_steps < len) p.warps *= 2;
-  double best = (double)up(p.tiles, slots * max_warps / p.warps) * (double)up(len, p.warps * warp_steps) * (aligned ? 3.6 : 0.95);
+  double best = (double)up(p.tiles, slots * max_warps / p.warps) * (double)(up(len, p.warps * warp_steps) + 1) * (aligned ? 3.6 : 0.95);
   const int64_t block = (int64_t)max_warps * 2 * kTileSteps;  // a wide block's steps
   const int64_t tiles = batch * up(channels, kWideChannels);
   const double round = aligned ? (grad ? 3.5 : 2.5) : (grad ? 10.0 : 5.0);
   // off alignment only large clusters are ever the better choice
   for (int cl = aligned ? 1 : 4; cl <= kMaxCluster && (cl == 1 || block * cl <= len); cl *= 2) {
-    const double cost = (double)up(tiles * cl, slots) * (double)up(len, block * cl) * round * (cl > 1 ? 1.1 : 1.0);
+    const double posts = cl == 1 ? 1.0 : cl == 2 ? 1.03 : cl == 4 ? 1.1 : 1.25;
+    const double cost = (double)up(tiles * cl, slots) * (double)(up(len, block * cl) + 1) * round * posts;
     if (cost < best) {
       best = cost;
       p.wide = true;
