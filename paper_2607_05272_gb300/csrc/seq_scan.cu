@@ -17,6 +17,7 @@
 // s -> A s + B across its threads (and, where there are few columns and many steps, across a cluster of
 // blocks that share the steps), and applies the state that comes in to the same registers.
 #include <algorithm>
+#include <initializer_list>
 
 #include "kernels.h"
 #include "seq_common.cuh"
@@ -575,11 +576,16 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
 constexpr int kWideLanes = 16, kWideChannels = 64, kWidePitch = 68;
 constexpr int kMaxCluster = 8;
 
-// Steps of 4 channels of K tensors on their way in the thread's places in shared memory.  ALIGNED: one copy
-// of 4 elements a step; else element by element, of the `count` channels that there are: asynchronously
-// for fp32, by way of registers for bf16 (all of a tensor's steps on their way at once).
-template <class T, int K, int S, bool ALIGNED>
+// How the wide tiles read and write 4 channels of a step: at once, by 4-byte words (fp32, and bf16 in pairs
+// of channels), or element by element.
+enum Access : int { WHOLE = 0, WORDS = 1, ELEMENTS = 2 };
+
+// Steps of 4 channels of K tensors on their way in the thread's places in shared memory, `count` channels
+// of them there.  Copies are asynchronous but for single bf16 elements, which come by way of registers (all
+// of a tensor's steps at once).
+template <class T, int K, int S, int ACCESS>
 struct WideAhead {
+  static constexpr int PER = ACCESS == WORDS ? 4 / (int)sizeof(T) : 1;  // elements per access
   T* slot;
   int pitch, count;
   __device__ __forceinline__ void start(void* shared) {
@@ -589,15 +595,15 @@ struct WideAhead {
   // Steps 0 .. steps - 1 at p, p + st, ...
   __device__ __forceinline__ void bring(int k, const T* p, int64_t st, int steps = S) {
     T* to = slot + k * S * pitch;
-    if (ALIGNED) {
+    if (ACCESS == WHOLE) {
 #pragma unroll
       for (int s = 0; s < S; ++s, p += st)
         if (s < steps) copy_async<4 * (int)sizeof(T)>(to + s * pitch, p);
-    } else if (sizeof(T) == 4) {
+    } else if (ACCESS == WORDS) {
 #pragma unroll
       for (int s = 0; s < S; ++s, p += st)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; i += PER)
           if (s < steps && i < count) copy_async<4>(to + s * pitch + i, p + i);
     } else {
       T v[S][4];
@@ -613,8 +619,12 @@ struct WideAhead {
   }
   __device__ __forceinline__ void take(int k, int s, float (&v)[4]) const { load_vec(slot + (k * S + s) * pitch, v); }
   __device__ __forceinline__ void put(T* p, const float (&v)[4]) const {
-    if (ALIGNED) {
+    if (ACCESS == WHOLE) {
       store_vec(p, v);
+    } else if (PER == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; i += 2)
+        if (i < count) *reinterpret_cast<uint32_t*>(p + i) = pack2(v[i], v[i + 1]);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -720,7 +730,7 @@ __device__ __forceinline__ uint32_t group_bits(uint8_t byte) {
   return __ballot_sync(0xffffffffu, byte != 0) >> ((int)threadIdx.x & 16) & 0xFFFFu;
 }
 
-template <class T, bool DONE, int CLT, bool ALIGNED>
+template <class T, bool DONE, int CLT, int ACCESS>
 __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles) {
   constexpr int S = kTileSteps, NW = 8, TB = 2 * NW * S;
   constexpr int64_t step = (int64_t)CLT * TB;
@@ -732,7 +742,7 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
   wide_start(sh);
   const int64_t per = (A.channels + kWideChannels - 1) / kWideChannels;
   const int64_t rounds = (A.len + step - 1) / step;
-  WideAhead<T, 2, S, ALIGNED> in;
+  WideAhead<T, 2, S, ACCESS> in;
   in.start(slots);
   uint32_t turn = 0;
   bool lost = false;
@@ -814,7 +824,7 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
 }
 
 // Backward, on the steps in reverse order; part [batch * CLT][channels]: sums of dgate (or null).
-template <class T, bool DONE, int CLT, bool ALIGNED>
+template <class T, bool DONE, int CLT, int ACCESS>
 __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t tiles, float* part) {
   constexpr int S = kTileSteps, NW = 4, TB = 2 * NW * S;
   constexpr int64_t step = (int64_t)CLT * TB;
@@ -827,7 +837,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
   wide_start(sh);
   const int64_t per = (A.channels + kWideChannels - 1) / kWideChannels;
   const int64_t rounds = (A.len + step - 1) / step;
-  WideAhead<T, 4, S, ALIGNED> in;
+  WideAhead<T, 4, S, ACCESS> in;
   in.start(slots);
   uint32_t turn = 0;
   bool lost = false;
@@ -972,8 +982,9 @@ struct ScanPlan {
   int lcl, warps, cluster;
   int64_t tiles;
 };
-ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, bool aligned, bool grad) {
+ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, int access, int dtype, bool grad) {
   ScanPlan p{};
+  const bool aligned = access == WHOLE;
   p.columns = len <= kColSteps;
   p.cluster = p.warps = 1;
   if (p.columns) return p;
@@ -987,9 +998,13 @@ ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, bool aligned, b
   double best = (double)up(p.tiles, slots * max_warps / p.warps) * (double)(up(len, p.warps * warp_steps) + 1) * (aligned ? 3.6 : 0.95);
   const int64_t block = (int64_t)max_warps * 2 * kTileSteps;  // a wide block's steps
   const int64_t tiles = batch * up(channels, kWideChannels);
-  const double round = aligned ? (grad ? 3.5 : 2.5) : (grad ? 10.0 : 5.0);
   // off alignment only large clusters are ever the better choice
   for (int cl = aligned ? 1 : 4; cl <= kMaxCluster && (cl == 1 || block * cl <= len); cl *= 2) {
+    // an SM with one block, and what the others add
+    const double full = std::min(1.0, (double)(tiles * cl) / (double)slots);
+    const double round = access == WHOLE ? (grad ? 3.5 : 2.5)
+                         : access == WORDS ? (grad ? (dtype == SIMX_F32 ? 4.0 + 6.0 * full : 4.0 + 3.0 * full) : (dtype == SIMX_F32 ? 2.5 + 2.5 * full : 2.5 + 1.5 * full))
+                                           : (grad ? 6.5 + 4.0 * full : 3.0 + 2.4 * full);
     const double posts = cl == 1 ? 1.0 : cl == 2 ? 1.03 : cl == 4 ? 1.1 : 1.25;
     const double cost = (double)up(tiles * cl, slots) * (double)(up(len, block * cl) + 1) * round * posts;
     if (cost < best) {
@@ -1002,10 +1017,19 @@ ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, bool aligned, b
   return p;
 }
 
+// How tensors of a call can be accessed.
 template <class T>
-bool vectors(const simx_scan& a, const simx_seq& q) {
-  const int64_t bytes = 4 * (int64_t)sizeof(T);
-  return (reinterpret_cast<uintptr_t>(q.p) % (uintptr_t)bytes) == 0 && (a.batch == 1 || q.sb % 4 == 0) && (a.len == 1 || q.st % 4 == 0);
+int access_of(const simx_scan& a, std::initializer_list<simx_seq> all) {
+  const int64_t es = (int64_t)sizeof(T);
+  const auto fits = [&](int64_t bytes) {
+    if (a.channels * es % bytes != 0) return false;
+    for (const simx_seq& q : all)
+      if ((int64_t)(reinterpret_cast<uintptr_t>(q.p) % (uintptr_t)bytes) != 0 || (a.batch > 1 && q.sb * es % bytes != 0) ||
+          (a.len > 1 && q.st * es % bytes != 0))
+        return false;
+    return true;
+  };
+  return a.len == 0 ? (a.channels % 4 == 0 ? WHOLE : ELEMENTS) : fits(4 * es) ? WHOLE : fits(4) ? WORDS : ELEMENTS;
 }
 
 template <class K, class... Args>
@@ -1030,78 +1054,87 @@ cudaError_t launch_tiles(K* kernel, const ScanPlan& p, int threads, size_t smem,
   return cudaLaunchKernelEx(&lc, kernel, args...);
 }
 
-template <class T, bool DONE, bool ALIGNED>
+template <class T, bool DONE, int ACCESS>
 cudaError_t scan_tiles(const simx_scan& a, const ScanPlan& p, cudaStream_t s) {
   if (p.wide) {
     const int th = 32 * kFwdWarps;
     const size_t smem = (size_t)th * 2 * kTileSteps * 4 * sizeof(T);
-    if (p.cluster == 8) return launch_tiles(k_scan_wide<T, DONE, 8, ALIGNED>, p, th, smem, s, a, p.tiles);
-    if (p.cluster == 4) return launch_tiles(k_scan_wide<T, DONE, 4, ALIGNED>, p, th, smem, s, a, p.tiles);
-    if constexpr (ALIGNED) {
-      if (p.cluster == 2) return launch_tiles(k_scan_wide<T, DONE, 2, true>, p, th, smem, s, a, p.tiles);
-      return launch_tiles(k_scan_wide<T, DONE, 1, true>, p, th, smem, s, a, p.tiles);
+    if (p.cluster == 8) return launch_tiles(k_scan_wide<T, DONE, 8, ACCESS>, p, th, smem, s, a, p.tiles);
+    if (p.cluster == 4) return launch_tiles(k_scan_wide<T, DONE, 4, ACCESS>, p, th, smem, s, a, p.tiles);
+    if constexpr (ACCESS == WHOLE) {
+      if (p.cluster == 2) return launch_tiles(k_scan_wide<T, DONE, 2, WHOLE>, p, th, smem, s, a, p.tiles);
+      return launch_tiles(k_scan_wide<T, DONE, 1, WHOLE>, p, th, smem, s, a, p.tiles);
     }
   }
-  const size_t smem = ALIGNED ? (size_t)p.warps * 32 * 2 * kTileSteps * 4 * sizeof(T) : 0;
-  return launch_tiles(k_scan_tiles<T, ALIGNED ? 4 : 1, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles);
+  constexpr int VEC = ACCESS == WHOLE ? 4 : 1;
+  const size_t smem = VEC == 4 ? (size_t)p.warps * 32 * 2 * kTileSteps * 4 * sizeof(T) : 0;
+  return launch_tiles(k_scan_tiles<T, VEC, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles);
 }
-template <class T, bool DONE, bool ALIGNED>
+template <class T, bool DONE, int ACCESS>
 cudaError_t scan_grad_tiles(const simx_scan& a, const ScanPlan& p, float* part, cudaStream_t s) {
   if (p.wide) {
     const int th = 32 * kGradWarps;
     const size_t smem = (size_t)th * 4 * kTileSteps * 4 * sizeof(T);
-    if (p.cluster == 8) return launch_tiles(k_scan_grad_wide<T, DONE, 8, ALIGNED>, p, th, smem, s, a, p.tiles, part);
-    if (p.cluster == 4) return launch_tiles(k_scan_grad_wide<T, DONE, 4, ALIGNED>, p, th, smem, s, a, p.tiles, part);
-    if constexpr (ALIGNED) {
-      if (p.cluster == 2) return launch_tiles(k_scan_grad_wide<T, DONE, 2, true>, p, th, smem, s, a, p.tiles, part);
-      return launch_tiles(k_scan_grad_wide<T, DONE, 1, true>, p, th, smem, s, a, p.tiles, part);
+    if (p.cluster == 8) return launch_tiles(k_scan_grad_wide<T, DONE, 8, ACCESS>, p, th, smem, s, a, p.tiles, part);
+    if (p.cluster == 4) return launch_tiles(k_scan_grad_wide<T, DONE, 4, ACCESS>, p, th, smem, s, a, p.tiles, part);
+    if constexpr (ACCESS == WHOLE) {
+      if (p.cluster == 2) return launch_tiles(k_scan_grad_wide<T, DONE, 2, WHOLE>, p, th, smem, s, a, p.tiles, part);
+      return launch_tiles(k_scan_grad_wide<T, DONE, 1, WHOLE>, p, th, smem, s, a, p.tiles, part);
     }
   }
-  const size_t smem = ALIGNED ? (size_t)p.warps * 32 * 4 * kTileSteps * 4 * sizeof(T) : 0;
-  return launch_tiles(k_scan_grad_tiles<T, ALIGNED ? 4 : 1, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles, part);
+  constexpr int VEC = ACCESS == WHOLE ? 4 : 1;
+  const size_t smem = VEC == 4 ? (size_t)p.warps * 32 * 4 * kTileSteps * 4 * sizeof(T) : 0;
+  return launch_tiles(k_scan_grad_tiles<T, VEC, DONE>, p, 32 * p.warps, smem, s, a, p.lcl, p.tiles, part);
 }
 
 template <class T>
 cudaError_t scan(const simx_scan& a, cudaStream_t s) {
-  const bool v4 = a.channels % 4 == 0 && (a.len == 0 || (vectors<T>(a, a.x) && vectors<T>(a, a.gate) && vectors<T>(a, a.h)));
-  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4, false);
+  const int access = access_of<T>(a, {a.x, a.gate, a.h});
+  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, access, a.dtype, false);
   if (p.columns) {
-    const int64_t cols = a.batch * (v4 ? a.channels / 4 : a.channels);
+    const int64_t cols = a.batch * (access == WHOLE ? a.channels / 4 : a.channels);
     const unsigned blocks = (unsigned)((cols + kColThreads - 1) / kColThreads);
-    if (v4) k_scan_columns<T, 4><<<blocks, kColThreads, 0, s>>>(a);
+    if (access == WHOLE) k_scan_columns<T, 4><<<blocks, kColThreads, 0, s>>>(a);
     else k_scan_columns<T, 1><<<blocks, kColThreads, 0, s>>>(a);
     count_launches(1);
     return cudaGetLastError();
   }
-  if (v4) return a.done ? scan_tiles<T, true, true>(a, p, s) : scan_tiles<T, false, true>(a, p, s);
-  return a.done ? scan_tiles<T, true, false>(a, p, s) : scan_tiles<T, false, false>(a, p, s);
+  if (access == WHOLE) return a.done ? scan_tiles<T, true, WHOLE>(a, p, s) : scan_tiles<T, false, WHOLE>(a, p, s);
+  if constexpr (sizeof(T) == 2) {
+    if (access == ELEMENTS) return a.done ? scan_tiles<T, true, ELEMENTS>(a, p, s) : scan_tiles<T, false, ELEMENTS>(a, p, s);
+  }
+  return a.done ? scan_tiles<T, true, WORDS>(a, p, s) : scan_tiles<T, false, WORDS>(a, p, s);
 }
 
 template <class T>
 cudaError_t scan_grad(const simx_scan& a, float* part, int64_t& rows, cudaStream_t s) {
-  const bool v4 = a.channels % 4 == 0 && (a.len == 0 || (vectors<T>(a, a.x) && vectors<T>(a, a.gate) && vectors<T>(a, a.h) &&
-                                                         vectors<T>(a, a.dh) && vectors<T>(a, a.dx) && vectors<T>(a, a.dgate)));
-  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, v4, true);
+  const int access = access_of<T>(a, {a.x, a.gate, a.h, a.dh, a.dx, a.dgate});
+  const ScanPlan p = plan_scan(a.batch, a.len, a.channels, access, a.dtype, true);
   rows = a.batch * p.cluster;
   if (p.columns) {
-    const int64_t cols = a.batch * (v4 ? a.channels / 4 : a.channels);
+    const int64_t cols = a.batch * (access == WHOLE ? a.channels / 4 : a.channels);
     const unsigned blocks = (unsigned)((cols + kColThreads - 1) / kColThreads);
-    if (v4) k_scan_grad_columns<T, 4><<<blocks, kColThreads, 0, s>>>(a, part);
+    if (access == WHOLE) k_scan_grad_columns<T, 4><<<blocks, kColThreads, 0, s>>>(a, part);
     else k_scan_grad_columns<T, 1><<<blocks, kColThreads, 0, s>>>(a, part);
     count_launches(1);
     return cudaGetLastError();
   }
-  if (v4) return a.done ? scan_grad_tiles<T, true, true>(a, p, part, s) : scan_grad_tiles<T, false, true>(a, p, part, s);
-  return a.done ? scan_grad_tiles<T, true, false>(a, p, part, s) : scan_grad_tiles<T, false, false>(a, p, part, s);
+  if (access == WHOLE) return a.done ? scan_grad_tiles<T, true, WHOLE>(a, p, part, s) : scan_grad_tiles<T, false, WHOLE>(a, p, part, s);
+  if constexpr (sizeof(T) == 2) {
+    if (access == ELEMENTS)
+      return a.done ? scan_grad_tiles<T, true, ELEMENTS>(a, p, part, s) : scan_grad_tiles<T, false, ELEMENTS>(a, p, part, s);
+  }
+  return a.done ? scan_grad_tiles<T, true, WORDS>(a, p, part, s) : scan_grad_tiles<T, false, WORDS>(a, p, part, s);
 }
 
 }  // namespace
 
 // The backward pass's sums of dgate: a row of channels per batch entry and block of a cluster, of whichever
-// plan the tensors' alignment gives.
+// plan the tensors' type and alignment give.
 size_t scan_workspace_bytes(int64_t batch, int64_t len, int64_t channels) {
-  const int cl = std::max(plan_scan(batch, len, channels, true, true).cluster,
-                          plan_scan(batch, len, channels, false, true).cluster);
+  int cl = 1;
+  for (int access : {WHOLE, WORDS, ELEMENTS})
+    for (int dtype : {SIMX_F32, SIMX_BF16}) cl = std::max(cl, plan_scan(batch, len, channels, access, dtype, true).cluster);
   return (size_t)batch * (size_t)cl * (size_t)channels * sizeof(float);
 }
 

@@ -425,3 +425,53 @@ def test_refusals(simx):
     refused(p, x, tok, start, st[:3], ws2, label_smoothing=1.5)
     refused(p, x, tok, start, st[:3], ws2, beta=float("nan"))
     refused(p, x, tok, start, st[:3], ws2, mask=torch.ones(4, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,V,ld", [(20, 70001, 70001), (20, 131072, 131072), (40, 33000, 33003)])
+def test_token_rows_enough_to_stream(simx, n, V, ld, dtype):
+    """Large vocabularies with more rows than go to clusters."""
+    _check_token(simx, n, V, dtype, n + V, ld=ld)
+
+
+@pytest.mark.parametrize("V", [70001, 131072])
+def test_token_streamed_rows_at_the_edges(simx, V):
+    """Masked, extreme, weightless and bad rows among streamed ones."""
+    rng = np.random.default_rng(V)
+    n, low = 24, float(np.finfo(np.float32).min)
+    x = rng.standard_normal((n, V)) * 2
+    x[0, 1:], x[1, ::2], x[2], x[3, ::3] = -np.inf, low, low, -np.inf
+    x[4], x[5, 7], x[6] = np.nan, np.inf, -np.inf
+    action = rng.integers(0, V, n)
+    action[:4] = [0, 1, 3, 1]
+    action[7] = -1
+    w = np.full(n, 0.25)
+    w[4:8] = 0.0
+    exact, grad, stats, lp, H = _token(simx, x, action, adv=_dev(np.ones(n)), weight=_dev(w), c_entropy=0.1, temperature=0.5)
+    z = np.clip(exact, -1e30, 1e30)
+    z[2], z[4:8] = 0.0, 0.0
+    action[4:8] = 0
+    with np.errstate(over="ignore"):
+        ref = seq.token_loss(z, action, np.ones(n), weight=w, c_entropy=0.1, temperature=0.5)
+    _close(grad, ref["grad"], ref["scale"])
+    _close(lp, ref["logp"], 1 + np.abs(ref["logp"]))
+    _close(stats, ref["stats"], ref["stats_scale"])
+    w[4:8] = 0.25
+    action[7] = -1
+    _, grad, stats, lp, _ = _token(simx, x, action, adv=_dev(np.ones(n)), weight=_dev(w))
+    assert np.isnan(grad[4:8]).all() and np.isfinite(np.delete(grad, range(4, 8), 0)).all() and np.isnan(stats[0])
+
+
+def test_preference_long_rows_extremes(simx):
+    """-inf and lowest-value masks among the logits, temperature off 1, rows that are their own pair."""
+    x, token, start, kw = _pref_case([2, 3, 1, 2], 40003, 19, "f32")
+    kw["mask"][:] = 1
+    keep = x[np.arange(len(token)), token].copy()
+    x[:, ::3], x[1:4, 1::3] = -np.inf, -3e38
+    x[np.arange(len(token)), token] = keep
+    grad, stats, ratio, margin = _pref(simx, x, token, start, kw, dict(beta=0.2, temperature=0.8), "f32")
+    z = np.maximum(_f64(torch.from_numpy(x).float()), -1e30)
+    ref = seq.preference_loss(z, token, start, beta=float(np.float32(0.2)), temperature=float(np.float32(0.8)), **kw)
+    _close(ratio, ref["ratio"], ref["ratio_scale"])
+    _close(stats, ref["stats"], ref["stats_scale"])
+    _close(grad, ref["grad"], ref["scale"])

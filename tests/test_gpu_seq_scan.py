@@ -322,3 +322,24 @@ def test_refusals(simx):
     refused(g, x, x, x, x, o(x), o(x), None, dbias=torch.zeros(6, device="cuda"))
     refused(g, x, x, x, x, None, o(x), ws)
     refused(g, x, x, x, x, o(x), o(x)[:, :, :5], ws)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [64, 66, 67, 130, 131])
+@pytest.mark.parametrize("layout", ["batch", "padded", "packed"])
+def test_clusters_of_every_access(simx, layout, C, dtype):
+    """Few columns and many steps: blocks of a cluster share them, whatever the channels' alignment."""
+    _check(simx, 1, 4500, C, dtype, layout, done=0.003)
+    _check(simx, 2, 1100, C, dtype, layout, offset=1)
+
+
+def test_clusters_with_the_state_in_place_and_ends_everywhere(simx):
+    for C in (64, 66, 67):
+        _check(simx, 1, 3000, C, "bf16", done=1.1)
+        c = _case(1, 5000, C, 31, 0.01)
+        x, gate, h = (_tensor((1, 5000, C), "bf16", "batch", v) for v in (c["x"], c["gate"], None))
+        state, last, dn = _dev(c["h0"]).clone(), torch.empty((1, C), device="cuda"), _done(c["done"], "batch")
+        simx.gated_scan(x, gate, h, h0=_dev(c["h0"]), done=dn, h_last=last)
+        simx.gated_scan(x, gate, h, h0=state, done=dn, h_last=state)
+        torch.cuda.synchronize()
+        assert torch.equal(state, last)
