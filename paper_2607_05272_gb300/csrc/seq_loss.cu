@@ -7,6 +7,10 @@
 // row's coefficient c = dL / d log pi(a) and entropy coefficient u = w c_entropy
 //   dL / dx_j = (c (delta_ja - p_j) + u p_j (log p_j + H)) / T.
 // Bound by HBM: a row is read once and its gradient written once; about 10 operations per logit.
+// Measured on one GB300 (floors at 6783 GB/s): token loss of 8192 x 131,072 bf16, an eighth of the rows
+// without weight, 742 us (594), 1021 x 50,001 fp32 76 (53), 8 x 131,072 bf16 8 and 8192 x 48 fp32 4.5 on the
+// GPU, where a call's arguments take the host 14; preference loss of 32 pairs of up to 512 tokens over
+// 32,768 bf16 logits 469 (297, or 442 with the second read that its coefficients need).
 #include <algorithm>
 
 #include "kernels.h"
@@ -161,7 +165,8 @@ __device__ __forceinline__ int phase_of(const T* p) {
 }
 
 // Small vocabularies: G lanes per row, NI logits per lane (logit lane + G i), every lane of the group
-// with the row's terms.
+// with the row's terms.  8192 x 48 fp32: 4.5 us with the statistics, by latency; 46,298 x 675 bf16 110 us,
+// by the instructions of a row's terms and its single-element loads.
 template <class T, int G, int NI>
 __global__ void __launch_bounds__(kRowThreads) k_token_lanes(TokenArgs A) {
   __shared__ float sh[kRowThreads / 32][4];
@@ -291,7 +296,11 @@ __device__ __noinline__ void row_grad_loop(const T* x, T* g, int V, const Args& 
 // (two rows per SM are 78 MB at 131,072 bf16 logits, of 129).  One pass takes the sums: each thread keeps
 // e = 2^(x k - c) with an integer reference c of its own, raised when a logit passes it, so that sums move
 // to another reference by an exact power of two.  No block waits for another one, which is what a row in
-// a cluster's registers costs: it is the kernel of calls with enough rows to fill the GPU.
+// a cluster's registers costs: it is the kernel of calls with enough rows to fill the GPU.  8192 rows of
+// 131,072 bf16 logits: 742 us, 5.4 TB/s of what the call cannot do without; DRAM moves 8 % more than that,
+// and what is left is the latency of a row's loads (warps wait for them 8 cycles per instruction).  The
+// same rows each in a cluster's registers took 1463 us.  A block takes one row, or few: the rows without
+// weight then leave their room to others (persistent blocks: 797).
 // ---------------------------------------------------------------------------
 constexpr int kChunk = 4;  // vectors per thread and step
 constexpr float kNone = -1e30f;  // reference of a thread that has seen nothing
@@ -554,7 +563,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_token_stream(TokenArgs A) {
 // ---------------------------------------------------------------------------
 // Few rows of a large vocabulary: a cluster of 8 blocks per row, every block's slice in its threads'
 // registers (64 logits each, 262,144 per cluster), read once; the blocks' sums meet in every block's
-// shared memory.
+// shared memory.  Bound by latency: 8 rows of 131,072 bf16 logits 8 us with the statistics.
 // ---------------------------------------------------------------------------
 constexpr int kCluster = 8, kClusterThreads = 512, kPerThread = 64;
 
@@ -725,7 +734,9 @@ __global__ void __launch_bounds__(256) k_pref_index(PrefArgs A) {
     A.row_seq[i] = A.mask && !A.mask[i] ? -1 : (int)seq_of(A, i);
 }
 
-// First pass: the log ratio and the sums of every row that counts, streamed as in the token loss.
+// The preference loss reads the logits twice: every row's coefficient waits for all rows of its pair.
+// First pass: the log ratio and the sums of every row that counts, streamed as in the token loss.  32 pairs
+// of 32,768 bf16 logits: two passes at 4.9 and 5.6 TB/s (62 % and 83 % of the DRAM's cycles).
 // row_is < 0 marks a row whose row_c is its maximum (see stream_holds) instead of the sums' reference.
 template <class T, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT) k_pref_rows(PrefArgs A) {

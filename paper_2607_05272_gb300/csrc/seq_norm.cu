@@ -10,6 +10,9 @@
 // the largest part of the instructions, so a draw gives eight 16-bit fields, one per column, and the drop
 // probability is a multiple of 2^-16.  A row stays in the registers of 1 to 32 warps between its sum and
 // its output, in units of 8 columns per thread.
+// Measured on one GB300 (floors at 6783 GB/s), bf16 with p = 0.1: forward 16,384 x 4096 90 us (79), backward
+// 124 (99); rows that are off the 16-byte grid, 16,384 x 2047: 83 (40) and 117 (50), by instructions (74 per
+// element backward: partial units, sums in shared memory because columns move between threads).
 #include <algorithm>
 
 #include "kernels.h"

@@ -16,6 +16,9 @@
 // element once: a block holds a tile of steps and channels in registers, joins the steps' maps
 // s -> A s + B across its threads (and, where there are few columns and many steps, across a cluster of
 // blocks that share the steps), and applies the state that comes in to the same registers.
+// Measured on one GB300 (floors at 6783 GB/s): forward 2 x 65,536 steps x 1024 channels bf16 165 us (119);
+// backward 1024 x 512 x 64 fp32, time-major with episode ends, 142 (119) and 16 x 2048 x 2048 bf16 162 (119);
+// one step of 256 x 2048 bf16 3.2 on the GPU, where the call's arguments take the host 11.5.
 #include <algorithm>
 #include <initializer_list>
 
@@ -571,7 +574,9 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_tiles(simx_scan A, int lcl
 // channel (NW / 2 neighbouring lanes per channel), joins them, and writes back the state before each
 // group.  That is a tenth of the instructions (the tile above takes 11 per element for it, of 40), for a
 // second barrier a round.  Where there are few tiles and many steps, a cluster of blocks shares the steps:
-// per round each block takes its part, in rank order, and posts its map to all others.
+// per round each block takes its part, in rank order, and posts its map to all others.  24 instructions per
+// element forward and 49 backward; what is left is the round's chain of barriers and posts at 16 and 12
+// warps per SM (2 x 65,536 x 1024 bf16: 54 % of the DRAM's cycles, half of the issue slots).
 // ---------------------------------------------------------------------------
 constexpr int kWideLanes = 16, kWideChannels = 64, kWidePitch = 68;
 constexpr int kMaxCluster = 8;
