@@ -165,7 +165,7 @@ __device__ __forceinline__ int phase_of(const T* p) {
 }
 
 // Small vocabularies: G lanes per row, NI logits per lane (logit lane + G i), every lane of the group
-// with the row's terms.  8192 x 48 fp32: 4.5 us with the statistics, by latency; 46,298 x 675 bf16 110 us,
+// with the row's terms.  8192 x 48 fp32: 4.5 us with the statistics, by latency; 65,536 x 500 bf16 83 us,
 // by the instructions of a row's terms and its single-element loads.
 template <class T, int G, int NI>
 __global__ void __launch_bounds__(kRowThreads) k_token_lanes(TokenArgs A) {
@@ -898,9 +898,10 @@ int stream_threads(int64_t V) {
   return bytes <= 8192 ? 32 : bytes <= 16384 ? 64 : bytes <= 32768 ? 128 : bytes <= 65536 ? 256 : 512;
 }
 
-// The kernel by the vocabulary: lane groups with 8 logits a lane, then a warp with 32, then streamed rows;
-// rows of 128 KB and more that are too few to fill the GPU, in clusters (131,072 bf16 logits, 8 rows: 19
-// against 26 us; at 19 rows, more than one wave of clusters, 26 against 25).
+// The kernel by the vocabulary: lane groups with 8 logits a lane, then a warp with 16 (65,536 rows of 500
+// bf16: 83 us against 93 streamed), then streamed rows (of 1024: 88 against 179 with 32 a lane); rows of 128
+// KB and more that are too few to fill the GPU, in clusters (131,072 bf16 logits, 8 rows: 19 against 26 us;
+// at 19 rows, more than one wave of clusters, 26 against 25).
 template <class T>
 cudaError_t token_rows(const TokenArgs& a, int& parts, cudaStream_t s) {
   if (a.V <= 32) return token_lanes<T, 4, 8>(a, parts, s);
@@ -908,7 +909,6 @@ cudaError_t token_rows(const TokenArgs& a, int& parts, cudaStream_t s) {
   if (a.V <= 128) return token_lanes<T, 16, 8>(a, parts, s);
   if (a.V <= 256) return token_lanes<T, 32, 8>(a, parts, s);
   if (a.V <= 512) return token_lanes<T, 32, 16>(a, parts, s);
-  if (a.V <= 1024) return token_lanes<T, 32, 32>(a, parts, s);
   const bool fits = a.V <= (int64_t)kCluster * kClusterThreads * kPerThread - 16 * VecOf<T>::N;
   if (fits && a.V * (int64_t)sizeof(T) >= 131072 && a.n * kCluster * 8 <= (int64_t)sm_count() * 7) return token_cluster<T>(a, parts, s);
   switch (stream_threads<T>(a.V)) {
