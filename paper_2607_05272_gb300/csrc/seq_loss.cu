@@ -101,8 +101,10 @@ __device__ __forceinline__ RowOut token_terms(const TokenArgs& A, const RowIn& i
   const float lp = l.value();
   float c = 0.0f;
   if (A.adv) {
-    const float rho = A.logp_old ? expf(l.minus(in.old)) : (lp == lp ? 1.0f : lp);
-    const float a = __fmul_rn(rho, in.adv);
+    const float d = A.logp_old ? l.minus(in.old) : 0.0f;
+    const float rho = A.logp_old ? expf(d) : (lp == lp ? 1.0f : lp);
+    // a ratio beyond fp32 is infinite here, but finite: times an advantage of 0 it is 0
+    const float a = in.adv == 0.0f && rho == inf() && d < inf() ? 0.0f : __fmul_rn(rho, in.adv);
     const float b = __fmul_rn(fminf(fmaxf(rho, A.lo), A.hi), in.adv);
     const bool clipped = b < a;
     terms[0] = __fmaf_rn(-w, clipped ? b : a, terms[0]);
@@ -114,7 +116,7 @@ __device__ __forceinline__ RowOut token_terms(const TokenArgs& A, const RowIn& i
     const float d = -l.minus(in.ref);
     const float em = expm1f(d);
     terms[1] = __fmaf_rn(w, __fsub_rn(em, d), terms[1]);
-    c = __fmaf_rn(-A.c_kl, em, c);
+    if (A.c_kl != 0.0f) c = __fmaf_rn(-A.c_kl, em, c);  // em may be beyond fp32
   }
   terms[2] = __fmaf_rn(w, o.H, terms[2]);
   o.c = __fmul_rn(__fmul_rn(c, w), it);
@@ -705,7 +707,7 @@ __global__ void __launch_bounds__(kStatThreads) k_token_stats(TokenArgs A, int p
   if (threadIdx.x < 4) A.stats[1 + q] = t.value();
   if (threadIdx.x == 0) {
     const float a = __fmul_rn(A.c_kl, kh), b = __fmul_rn(-A.c_entropy, eh);
-    t.add(a, __fmaf_rn(A.c_kl, kl, __fmaf_rn(A.c_kl, kh, -a)));
+    if (A.c_kl != 0.0f) t.add(a, __fmaf_rn(A.c_kl, kl, __fmaf_rn(A.c_kl, kh, -a)));
     t.add(b, __fmaf_rn(-A.c_entropy, el, __fmaf_rn(-A.c_entropy, eh, -b)));
     A.stats[0] = t.value();
   }

@@ -475,3 +475,24 @@ def test_preference_long_rows_extremes(simx):
     _close(ratio, ref["ratio"], ref["ratio_scale"])
     _close(stats, ref["stats"], ref["stats_scale"])
     _close(grad, ref["grad"], ref["scale"])
+
+
+@pytest.mark.parametrize("V", [50, 700, 5000, 131072])
+def test_token_ratios_beyond_fp32(simx, V):
+    """exp(lp - logp_old) and exp(logp_ref - lp) overflow fp32: an advantage of zero, a ratio that is clipped and a
+    KL term of coefficient zero take nothing from them; only the KL itself is infinite."""
+    x, action, kw = _inputs(3, V, V, masked=0.0)
+    x = _f64(torch.from_numpy(x).float())
+    f = lambda v: v.astype(np.float32).astype(np.float64)  # noqa: E731
+    lp = np.take_along_axis(seq.log_softmax(x), action[:, None], 1)[:, 0]
+    kw = dict(adv=np.array([0.0, 1.5, -0.5]), logp_old=f(lp - np.array([95.0, 95.0, 0.1])),
+              logp_ref=f(lp + np.array([95.0, 0.1, 0.2])), weight=np.array([0.5, 0.25, 0.25]))
+    par = dict(clip_low=0.2, clip_high=0.3, c_kl=0.0, c_entropy=0.02)
+    _, grad, stats, glp, H = _token(simx, x, action, **{k: _dev(v) for k, v in kw.items()}, **par)
+    ref = seq.token_loss(x, action, **kw, **par)
+    # a clipped ratio adds nothing to the gradient and its bound to the loss, whatever the ratio
+    size = seq.token_loss(x, action, **dict(kw, adv=np.array([0.0, 0.0, -0.5])), **par)
+    _close(grad, ref["grad"], size["scale"])
+    keep = [0, 1, 3, 4]
+    _close(stats[keep], ref["stats"][keep], (size["stats_scale"] + 0.25 * 1.3 * 1.5)[keep])
+    assert stats[2] == np.inf
