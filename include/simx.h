@@ -539,6 +539,7 @@ simx_status simx_token_loss_grad(const simx_logits* x, const simx_token_loss* lo
  *   L = sum_p w_p ( (1 - label_smoothing) softplus(-margin_p) + label_smoothing softplus(margin_p) ).
  * mask NULL: every row counts; logp_ref NULL: zeros; weight NULL: 1 / pairs.  Rows that are masked or
  * belong to no sequence count for nothing, whatever they hold, and their gradient rows are zeros.
+ * Neither does a pair of weight 0, save that its ratios and margin are reported.
  * stats [3] = {L, sum w [margin > 0], sum w margin}; ratio [2 pairs], margin [pairs]: may be NULL.
  * pairs == 0: stats and every gradient row are zeros.
  */

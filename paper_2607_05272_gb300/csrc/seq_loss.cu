@@ -800,10 +800,11 @@ __global__ void __launch_bounds__(256) k_pref_pairs(PrefArgs A) {
       const float w = A.weight ? A.weight[p] : A.w_all;
       const double sg = 1.0 / (1.0 + exp(-h));
       const double eps = (double)A.smoothing;
+      const bool on = w != 0.0f;  // a pair of weight 0 counts for nothing, whatever its rows hold
       A.coef[p] = (float)((double)w * (double)A.beta * (sg - (1.0 - eps)) * (double)A.inv_t);
-      A.part[3 * p] = (double)w * ((1.0 - eps) * lneg + (eps > 0.0 ? eps * lpos : 0.0));
+      A.part[3 * p] = on ? (double)w * ((eps < 1.0 ? (1.0 - eps) * lneg : 0.0) + (eps > 0.0 ? eps * lpos : 0.0)) : 0.0;
       A.part[3 * p + 1] = h > 0.0 ? (double)w : 0.0;
-      A.part[3 * p + 2] = (double)w * h;
+      A.part[3 * p + 2] = on ? (double)w * h : 0.0;
       if (A.ratio) {
         A.ratio[2 * p] = (float)r[0];
         A.ratio[2 * p + 1] = (float)r[1];
@@ -834,7 +835,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_pref_grad(PrefArgs A) {
   for (int64_t i = A.n - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
     T* g = static_cast<T*>(A.g) + i * A.g_ld;
     const int q = A.pairs > 0 ? A.row_seq[i] : -1;
-    if (q < 0) {
+    if (q < 0 || (A.weight && A.weight[q >> 1] == 0.0f)) {
       zero_row<T, NT>(g, V);
       continue;
     }

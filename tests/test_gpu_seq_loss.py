@@ -496,3 +496,17 @@ def test_token_ratios_beyond_fp32(simx, V):
     keep = [0, 1, 3, 4]
     _close(stats[keep], ref["stats"][keep], (size["stats_scale"] + 0.25 * 1.3 * 1.5)[keep])
     assert stats[2] == np.inf
+
+
+@pytest.mark.parametrize("V", [60, 5000, 70000])
+def test_preference_pairs_without_weight_count_for_nothing(simx, V):
+    x, token, start, kw = _pref_case([4, 4, 3, 5], V, 7, "f32")
+    kw["mask"][:] = 1
+    kw["weight"][0] = 0.0
+    ref = seq.preference_loss(x, token, start, beta=float(np.float32(0.1)), **kw)
+    x[:3] = np.nan
+    token[5] = -1
+    grad, stats, ratio, margin = _pref(simx, x, token, start, kw, dict(beta=0.1), "f32")
+    assert not grad[:8].any() and np.isnan(margin[0]) and np.isnan(ratio[:2]).all()
+    _close(grad[8:], ref["grad"][8:], ref["scale"][8:])
+    _close(stats, ref["stats"], ref["stats_scale"])
