@@ -8,6 +8,7 @@
 #include <cstdio>
 #include <atomic>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 
@@ -924,6 +925,13 @@ static simx_status check_workspace(const void* p, size_t given, size_t need) {
   return SIMX_OK;
 }
 
+// Whether every one of the pointers (NULL among them) is a multiple of `bytes`.
+static simx_status check_aligned(std::initializer_list<const void*> all, int bytes) {
+  uintptr_t low = 0;
+  for (const void* p : all) low |= reinterpret_cast<uintptr_t>(p);
+  return low & (uintptr_t)(bytes - 1) ? fail(SIMX_EINVAL, "a pointer to %d-byte elements is misaligned", bytes) : SIMX_OK;
+}
+
 static simx_status check_logits(const simx_logits* x) {
   if (!x) return fail(SIMX_EINVAL, "logits are NULL");
   const int es = elem_bytes(x->dtype);
@@ -952,6 +960,8 @@ simx_status simx_token_loss_grad(const simx_logits* x, const simx_token_loss* l,
   if (!(l->clip_low >= 0.0f) || !(l->clip_high >= 0.0f) || !std::isfinite(l->clip_low) || !std::isfinite(l->clip_high))
     return fail(SIMX_EINVAL, "clip range %g, %g", (double)l->clip_low, (double)l->clip_high);
   if (!std::isfinite(l->c_kl) || !std::isfinite(l->c_entropy)) return fail(SIMX_EINVAL, "c_kl or c_entropy is not finite");
+  if ((v = check_aligned({l->action}, 8)) != SIMX_OK) return v;
+  if ((v = check_aligned({l->adv, l->logp_old, l->logp_ref, l->weight, l->logp, l->entropy, l->stats}, 4)) != SIMX_OK) return v;
   v = check_workspace(d_workspace, workspace_bytes, token_workspace_bytes(x->n));
   if (v != SIMX_OK) return v;
   TokenArgs a;
@@ -998,6 +1008,8 @@ simx_status simx_preference_loss_grad(const simx_logits* x, const simx_preferenc
   if (l->pairs > 0 && (!l->seq_start || (x->n > 0 && !l->token))) return fail(SIMX_EINVAL, "tokens and sequence starts are required");
   if (!std::isfinite(l->beta)) return fail(SIMX_EINVAL, "beta is not finite");
   if (!(l->label_smoothing >= 0.0f) || !(l->label_smoothing <= 1.0f)) return fail(SIMX_EINVAL, "label smoothing %g", (double)l->label_smoothing);
+  if ((v = check_aligned({l->token, l->seq_start}, 8)) != SIMX_OK) return v;
+  if ((v = check_aligned({l->logp_ref, l->weight, l->ratio, l->margin, l->stats}, 4)) != SIMX_OK) return v;
   v = check_workspace(d_workspace, workspace_bytes, pref_workspace_bytes(x->n, l->pairs));
   if (v != SIMX_OK) return v;
   PrefArgs a;
@@ -1052,7 +1064,9 @@ static simx_status check_scan(const simx_scan* s) {
   if (s->batch < 0 || s->len < 0 || s->channels < 0 || s->batch > most || s->channels > most || s->len > most ||
       (double)s->batch * (double)s->channels > 68719476736.0)
     return fail(SIMX_EINVAL, "batch %lld, len %lld, channels %lld", (long long)s->batch, (long long)s->len, (long long)s->channels);
-  return SIMX_OK;
+  if (s->done && (s->done_sb < 0 || s->done_st < 0 || s->done_sb > kMaxRows || s->done_st > kMaxRows))
+    return fail(SIMX_EINVAL, "strides of done: %lld, %lld", (long long)s->done_sb, (long long)s->done_st);
+  return check_aligned({s->bias, s->h0, s->h_last, s->dh_last, s->dbias, s->dh0}, 4);
 }
 
 size_t simx_gated_scan_workspace_size(int64_t batch, int64_t len, int64_t channels) {
@@ -1113,7 +1127,7 @@ static simx_status check_norm(const simx_norm* a) {
     return fail(SIMX_EINVAL, "%lld rows from row %u on", (long long)a->n, a->row_base);
   if (!(a->p >= 0.0f) || !((double)a->p * 65536.0 + 0.5 < 65536.0)) return fail(SIMX_EINVAL, "drop probability %g", (double)a->p);
   if (a->n > 0 && !a->gain) return fail(SIMX_EINVAL, "gain is NULL");
-  return SIMX_OK;
+  return check_aligned({a->gain, a->rstd, a->dgain}, 4);
 }
 
 simx_status simx_dropout_add_norm(const simx_norm* a, void* stream) {

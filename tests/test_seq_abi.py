@@ -172,3 +172,40 @@ def test_binding_refuses_host_tensors(lib):
         with pytest.raises(simx.SimxError) as e:
             call()
         assert e.value.status == simx.EINVAL
+
+
+@pytest.mark.parametrize("name,ptr", [
+    ("action", 4), ("adv", 2), ("logp_old", 1), ("logp_ref", 2), ("weight", 2), ("logp", 3), ("entropy", 2), ("stats", 2)])
+def test_misaligned_rows_of_the_token_loss(lib, name, ptr):
+    a, b = _logits(), _token(**{name: FAKE + ptr})
+    _refused(lib, lib.simx_token_loss_grad(C.byref(a), C.byref(b), FAKE, 1 << 30, None))
+
+
+@pytest.mark.parametrize("name,ptr", [
+    ("token", 4), ("seq_start", 4), ("logp_ref", 2), ("weight", 2), ("ratio", 1), ("margin", 2), ("stats", 3)])
+def test_misaligned_rows_of_the_preference_loss(lib, name, ptr):
+    d = dict(token=FAKE, seq_start=FAKE, pairs=2, beta=0.1, stats=FAKE)
+    d[name] = FAKE + ptr
+    a, b = _logits(), simx.PreferenceLoss(**d)
+    _refused(lib, lib.simx_preference_loss_grad(C.byref(a), C.byref(b), FAKE, 1 << 30, None))
+
+
+@pytest.mark.parametrize("name", ["bias", "h0", "h_last", "dh_last", "dbias", "dh0"])
+def test_misaligned_states_of_the_scan(lib, name):
+    s = _scan(**{name: FAKE + 2})
+    _refused(lib, lib.simx_gated_scan(C.byref(s), None, 0, None))
+    _refused(lib, lib.simx_gated_scan_grad(C.byref(s), FAKE, 1 << 30, None))
+
+
+@pytest.mark.parametrize("name", ["gain", "rstd", "dgain"])
+def test_misaligned_rows_of_the_norm(lib, name):
+    a = _norm(**{name: FAKE + 2})
+    _refused(lib, lib.simx_dropout_add_norm(C.byref(a), None))
+    _refused(lib, lib.simx_dropout_add_norm_grad(C.byref(a), FAKE, 1 << 30, None))
+
+
+@pytest.mark.parametrize("sb,st", [(-4, 1), (4, -1), (1 << 41, 1), (4, 1 << 41)])
+def test_strides_of_episode_ends(lib, sb, st):
+    s = _scan(done=FAKE, done_sb=sb, done_st=st)
+    _refused(lib, lib.simx_gated_scan(C.byref(s), None, 0, None))
+    _refused(lib, lib.simx_gated_scan_grad(C.byref(s), FAKE, 1 << 30, None))
