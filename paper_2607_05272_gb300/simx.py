@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 import threading
 
 import numpy as np
@@ -537,10 +538,32 @@ def _refuse(msg: str):
     raise SimxError(EINVAL, msg)
 
 
+def _image(cls):
+    """A function from a structure's fields, in order and nested ones flattened, to its bytes (pointers
+    as integers).  Packing takes a quarter of the time of filling the ctypes structure."""
+    def codes(c):
+        return "".join(codes(f[1]) if issubclass(f[1], C.Structure) else f[1]._type_ for f in c._fields_)
+    # "l" and "L" of ctypes' 64-bit integers are 64 bits in native layout too
+    layout = struct.Struct("@" + codes(cls) + "0q")
+    assert layout.size == C.sizeof(cls)
+    pack = layout.pack
+
+    def image(*values):
+        try:
+            return pack(*values)
+        except (struct.error, OverflowError) as e:
+            _refuse("argument out of range: %s" % e)
+    return image
+
+
+_logits_image, _token_loss_image = _image(Logits), _image(TokenLoss)
+_preference_loss_image, _scan_image, _norm_image = _image(PreferenceLoss), _image(Scan), _image(Norm)
+
+
 def _tensor(t, name: str, like, shape, dev: int):
     """A data tensor: `like`'s dtype, `shape`, on device `dev`, unit stride along the last axis."""
     if t is None:
-        return None
+        return 0
     if t.dtype is not like.dtype or t.shape != shape or t.get_device() != dev:
         _refuse("%s: %s %s on %s expected, got %s %s on %s" % (
             name, tuple(shape), like.dtype, like.device, tuple(t.shape), t.dtype, t.device))
@@ -552,7 +575,7 @@ def _tensor(t, name: str, like, shape, dev: int):
 def _flat(t, name: str, dtype, shape, dev: int):
     """A contiguous tensor of `dtype` and `shape` on device `dev`."""
     if t is None:
-        return None
+        return 0
     if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         _refuse("%s: contiguous %s %s on cuda:%d expected, got %s %s on %s" % (
             name, tuple(shape), dtype, dev, tuple(t.shape), t.dtype, t.device))
@@ -593,10 +616,10 @@ def _ld(t, shape) -> int:
 def _logits(logits, grad, temperature):
     torch, dt, shape, dev = _dtype(logits, "logits", 2)
     n, vocab = shape
-    return torch, dev, n, Logits(_tensor(logits, "logits", logits, shape, dev),
-                                 _tensor(grad, "grad", logits, shape, dev), _ld(logits, shape),
-                                 _ld(grad, shape) if grad is not None else 0, n, vocab, dt,
-                                 temperature)
+    return torch, dev, n, _logits_image(_tensor(logits, "logits", logits, shape, dev),
+                                        _tensor(grad, "grad", logits, shape, dev),
+                                        _ld(logits, shape), _ld(grad, shape) if grad is not None else 0,
+                                        n, vocab, dt, temperature)
 
 
 def token_loss_grad_workspace_size(n: int) -> int:
@@ -613,13 +636,13 @@ def token_loss_grad(logits, action, adv, stats, workspace, logp_old=None, logp_r
     clipped share; grad: like logits, logits itself, or None."""
     torch, dev, n, x = _logits(logits, grad, temperature)
     n, f = (n,), torch.float32
-    a = TokenLoss(_flat(action, "action", torch.int64, n, dev), _flat(adv, "adv", f, n, dev),
-                  _flat(logp_old, "logp_old", f, n, dev), _flat(logp_ref, "logp_ref", f, n, dev),
-                  _flat(weight, "weight", f, n, dev), clip_low, clip_high, c_kl, c_entropy,
-                  _flat(logp, "logp", f, n, dev), _flat(entropy, "entropy", f, n, dev),
-                  _flat(stats, "stats", f, (5,), dev))
-    _check(lib().simx_token_loss_grad(C.byref(x), C.byref(a), *_workspace(workspace, dev),
-                                      _stream(stream)))
+    a = _token_loss_image(
+        _flat(action, "action", torch.int64, n, dev), _flat(adv, "adv", f, n, dev),
+        _flat(logp_old, "logp_old", f, n, dev), _flat(logp_ref, "logp_ref", f, n, dev),
+        _flat(weight, "weight", f, n, dev), clip_low, clip_high, c_kl, c_entropy,
+        _flat(logp, "logp", f, n, dev), _flat(entropy, "entropy", f, n, dev),
+        _flat(stats, "stats", f, (5,), dev))
+    _check(lib().simx_token_loss_grad(x, a, *_workspace(workspace, dev), _stream(stream)))
 
 
 def preference_loss_grad_workspace_size(n: int, pairs: int) -> int:
@@ -639,15 +662,14 @@ def preference_loss_grad(logits, token, seq_start, stats, workspace, logp_ref=No
     if seq_start is None or seq_start.dim() != 1 or len(seq_start) % 2 != 1:
         _refuse("seq_start: 2 * pairs + 1 row offsets expected")
     pairs = len(seq_start) // 2
-    a = PreferenceLoss(_flat(token, "token", torch.int64, n, dev),
-                       _flat(seq_start, "seq_start", torch.int64, seq_start.shape, dev),
-                       _flat(mask, "mask", torch.uint8, n, dev),
-                       _flat(logp_ref, "logp_ref", f, n, dev),
-                       _flat(weight, "weight", f, (pairs,), dev), pairs, beta, label_smoothing,
-                       _flat(ratio, "ratio", f, (2 * pairs,), dev),
-                       _flat(margin, "margin", f, (pairs,), dev), _flat(stats, "stats", f, (3,), dev))
-    _check(lib().simx_preference_loss_grad(C.byref(x), C.byref(a), *_workspace(workspace, dev),
-                                           _stream(stream)))
+    a = _preference_loss_image(
+        _flat(token, "token", torch.int64, n, dev),
+        _flat(seq_start, "seq_start", torch.int64, seq_start.shape, dev),
+        _flat(mask, "mask", torch.uint8, n, dev), _flat(logp_ref, "logp_ref", f, n, dev),
+        _flat(weight, "weight", f, (pairs,), dev), pairs, beta, label_smoothing,
+        _flat(ratio, "ratio", f, (2 * pairs,), dev), _flat(margin, "margin", f, (pairs,), dev),
+        _flat(stats, "stats", f, (3,), dev))
+    _check(lib().simx_preference_loss_grad(x, a, *_workspace(workspace, dev), _stream(stream)))
 
 
 def gated_scan_workspace_size(batch: int, length: int, channels: int) -> int:
@@ -655,28 +677,29 @@ def gated_scan_workspace_size(batch: int, length: int, channels: int) -> int:
 
 
 def _seq(t, name: str, like, shape, dev: int):
-    """A Seq of a tensor of `like`'s dtype."""
+    """The fields of a Seq of a tensor of `like`'s dtype."""
     p = _tensor(t, name, like, shape, dev)
     if t is None:
-        return Seq()
+        return 0, 0, 0
     sb, st, _ = t.stride()
-    return Seq(p, sb, st)
+    return p, sb, st
 
 
 def _scan(x, gate, h, bias, h0, done):
+    """Shape and device of a scan, and the fields of its Scan before h_last."""
     torch, dt, shape, dev = _dtype(x, "x", 3)
     b, t, c = shape
-    d, dsb, dst = None, 0, 0
+    d, dsb, dst = 0, 0, 0
     if done is not None:
         if done.dtype is not torch.uint8 or done.shape != (b, t) or done.get_device() != dev:
             _refuse("done: uint8 %s on cuda:%d expected" % ((b, t), dev))
         d = done.data_ptr()
         dsb, dst = done.stride()
     f = torch.float32
-    return f, shape, dev, Scan(b, t, c, dt, _seq(x, "x", x, shape, dev),
-                               _seq(gate, "gate", x, shape, dev), _seq(h, "h", x, shape, dev),
-                               _flat(bias, "bias", f, (c,), dev),
-                               _flat(h0, "h0", f, (b, c), dev), d, dsb, dst)
+    return f, shape, dev, (b, t, c, dt, *_seq(x, "x", x, shape, dev),
+                           *_seq(gate, "gate", x, shape, dev), *_seq(h, "h", x, shape, dev),
+                           _flat(bias, "bias", f, (c,), dev), _flat(h0, "h0", f, (b, c), dev),
+                           d, dsb, dst)
 
 
 def gated_scan(x, gate, h, workspace=None, bias=None, h0=None, done=None, h_last=None, stream=None):
@@ -684,28 +707,26 @@ def gated_scan(x, gate, h, workspace=None, bias=None, h0=None, done=None, h_last
     [batch, len, channels] of any batch and time strides (simx_gated_scan).  bias: fp32 [channels];
     h0, h_last: fp32 [batch, channels] (h_last may be h0: the single-token step of serving); done:
     uint8 [batch, len], nonzero where the state is not carried on; each of them may be None."""
-    f, (b, _, c), dev, s = _scan(x, gate, h, bias, h0, done)
-    s.h_last = _flat(h_last, "h_last", f, (b, c), dev)
-    _check(lib().simx_gated_scan(C.byref(s), *_workspace(workspace, dev), _stream(stream)))
+    f, (b, _, c), dev, head = _scan(x, gate, h, bias, h0, done)
+    s = _scan_image(*head, _flat(h_last, "h_last", f, (b, c), dev), *(0,) * 12)
+    _check(lib().simx_gated_scan(s, *_workspace(workspace, dev), _stream(stream)))
 
 
 def gated_scan_grad(x, gate, h, dh, dx, dgate, workspace, bias=None, h0=None, done=None,
                     dh_last=None, dbias=None, dh0=None, stream=None):
     """The backward pass of gated_scan (simx_gated_scan_grad): dx, dgate and, where given, dbias
     and dh0 from dh and dh_last, with h as the forward pass left it."""
-    f, shape, dev, s = _scan(x, gate, h, bias, h0, done)
+    f, shape, dev, head = _scan(x, gate, h, bias, h0, done)
     state = (shape[0], shape[2])
-    s.dh, s.dx = _seq(dh, "dh", x, shape, dev), _seq(dx, "dx", x, shape, dev)
-    s.dgate = _seq(dgate, "dgate", x, shape, dev)
-    s.dh_last = _flat(dh_last, "dh_last", f, state, dev)
-    s.dbias = _flat(dbias, "dbias", f, state[1:], dev)
-    s.dh0 = _flat(dh0, "dh0", f, state, dev)
-    _check(lib().simx_gated_scan_grad(C.byref(s), *_workspace(workspace, dev), _stream(stream)))
+    s = _scan_image(*head, 0, *_seq(dh, "dh", x, shape, dev), *_seq(dx, "dx", x, shape, dev),
+                    *_seq(dgate, "dgate", x, shape, dev), _flat(dh_last, "dh_last", f, state, dev),
+                    _flat(dbias, "dbias", f, state[1:], dev), _flat(dh0, "dh0", f, state, dev))
+    _check(lib().simx_gated_scan_grad(s, *_workspace(workspace, dev), _stream(stream)))
 
 
 def _rows(t, name: str, like, shape, dev: int):
     """(pointer, row stride) of a tensor of `like`'s dtype."""
-    return (_tensor(t, name, like, shape, dev), _ld(t, shape)) if t is not None else (None, 0)
+    return (_tensor(t, name, like, shape, dev), _ld(t, shape)) if t is not None else (0, 0)
 
 
 def _norm(like, name: str, gain, rstd, p, eps, seed, step, row_base):
@@ -725,9 +746,9 @@ def dropout_add_norm(x, gain, y, residual=None, z=None, rstd=None, p: float = 0.
     (simx_dropout_add_norm).  The mask is a function of (seed, step, row_base + row, column) and is
     not stored.  gain: fp32 [width]; rstd: fp32 [n] or None, kept for the backward pass."""
     _, n, dev, head = _norm(x, "x", gain, rstd, p, eps, seed, step, row_base)
-    a = Norm(*head, *_rows(x, "x", x, n, dev), *_rows(residual, "residual", x, n, dev),
-             *_rows(z, "z", x, n, dev), *_rows(y, "y", x, n, dev))
-    _check(lib().simx_dropout_add_norm(C.byref(a), _stream(stream)))
+    a = _norm_image(*head, *_rows(x, "x", x, n, dev), *_rows(residual, "residual", x, n, dev),
+                    *_rows(z, "z", x, n, dev), *_rows(y, "y", x, n, dev), *(0,) * 9)
+    _check(lib().simx_dropout_add_norm(a, _stream(stream)))
 
 
 def dropout_add_norm_grad_workspace_size(n: int, width: int) -> int:
@@ -741,10 +762,10 @@ def dropout_add_norm_grad(z, gain, rstd, dy, dx, workspace, dz=None, dresidual=N
     (each may be None) from dy and dz, with z and rstd as the forward pass left them and the same
     p, seed, step and row_base."""
     f, n, dev, head = _norm(z, "z", gain, rstd, p, 0.0, seed, step, row_base)
-    a = Norm(*head, None, 0, None, 0, *_rows(z, "z", z, n, dev), None, 0,
-             *_rows(dy, "dy", z, n, dev), *_rows(dz, "dz", z, n, dev), *_rows(dx, "dx", z, n, dev),
-             *_rows(dresidual, "dresidual", z, n, dev), _flat(dgain, "dgain", f, n[1:], dev))
-    _check(lib().simx_dropout_add_norm_grad(C.byref(a), *_workspace(workspace, dev), _stream(stream)))
+    a = _norm_image(*head, 0, 0, 0, 0, *_rows(z, "z", z, n, dev), 0, 0, *_rows(dy, "dy", z, n, dev),
+                    *_rows(dz, "dz", z, n, dev), *_rows(dx, "dx", z, n, dev),
+                    *_rows(dresidual, "dresidual", z, n, dev), _flat(dgain, "dgain", f, n[1:], dev))
+    _check(lib().simx_dropout_add_norm_grad(a, *_workspace(workspace, dev), _stream(stream)))
 
 
 def fma_probe_sink_floats() -> int:

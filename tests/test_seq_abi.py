@@ -209,3 +209,21 @@ def test_strides_of_episode_ends(lib, sb, st):
     s = _scan(done=FAKE, done_sb=sb, done_st=st)
     _refused(lib, lib.simx_gated_scan(C.byref(s), None, 0, None))
     _refused(lib, lib.simx_gated_scan_grad(C.byref(s), FAKE, 1 << 30, None))
+
+
+def _leaves(value):
+    for name, kind in type(value)._fields_:
+        v = getattr(value, name)
+        yield from _leaves(v) if issubclass(kind, C.Structure) else [v]
+
+
+@pytest.mark.parametrize("image,cls", [
+    (simx._logits_image, simx.Logits), (simx._token_loss_image, simx.TokenLoss),
+    (simx._preference_loss_image, simx.PreferenceLoss), (simx._scan_image, simx.Scan), (simx._norm_image, simx.Norm)])
+def test_packed_images_are_the_structures(image, cls):
+    n = len(list(_leaves(cls())))
+    assert list(_leaves(cls.from_buffer_copy(image(*range(1, n + 1))))) == list(range(1, n + 1))
+    for bad in (1e40, 1 << 70, "x"):  # beyond every field, or no number
+        with pytest.raises(simx.SimxError) as e:
+            image(*[bad] * n)
+        assert e.value.status == simx.EINVAL
