@@ -9,7 +9,7 @@
 // Bound by HBM: a row is read once and its gradient written once; about 10 operations per logit.
 // Measured on one GB300 (floors at 6783 GB/s): token loss of 8192 x 131,072 bf16, an eighth of the rows
 // without weight, 742 us (594), 1021 x 50,001 fp32 76 (53), 8 x 131,072 bf16 8 and 8192 x 48 fp32 4.5 on the
-// GPU, where a call's arguments take the host 14; preference loss of 32 pairs of up to 512 tokens over
+// GPU, where a call's arguments take the host 13; preference loss of 32 pairs of up to 512 tokens over
 // 32,768 bf16 logits 469 (297, or 442 with the second read that its coefficients need).
 #include <algorithm>
 
