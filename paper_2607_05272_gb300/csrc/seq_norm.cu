@@ -521,7 +521,7 @@ cudaError_t launch_norm_grad(const simx_norm& a, void* ws, cudaStream_t s) {
     lc.attrs = at;
     lc.numAttrs = 1;
   }
-  if (!slab) return cudaSuccess;
+  if (!a.dgain) return cudaSuccess;  // not `slab`: without rows the workspace has no bytes, and may be NULL
   lc.gridDim = dim3((unsigned)((a.width + 31) / 32));
   lc.blockDim = dim3(1024);
   lc.stream = s;

@@ -280,3 +280,15 @@ def test_refusals(simx):
     refused(g, x, gain, r, None, o(x), ws)
     refused(g, x, gain, r, x, o(x), ws[:8], dgain=gain.clone())
     refused(g, x, gain, r, x, o(x), None, dgain=gain.clone())
+
+
+@pytest.mark.parametrize("W", [40, 16384])
+def test_gain_gradient_of_no_rows_with_the_workspace_asked_for(simx, W):
+    """The size function asks for 0 bytes, so the workspace may be an empty tensor or None."""
+    e, gain, r = torch.empty((0, W), device="cuda"), torch.ones(W, device="cuda"), torch.empty(0, device="cuda")
+    size = simx.dropout_add_norm_grad_workspace_size(0, W)
+    for ws in (torch.empty(size, dtype=torch.uint8, device="cuda"), None):
+        d = torch.ones(W, device="cuda")
+        simx.dropout_add_norm_grad(e, gain, r, e, None, ws, dgain=d)
+        torch.cuda.synchronize()
+        assert not d.any()
