@@ -43,6 +43,7 @@ struct LogP {
   float hi, lo;   // log pi(token)
   float logs;     // log s, rounded
   float H;        // entropy
+  bool never;     // the token's logit is -inf
   __device__ __forceinline__ float value() const { return __fadd_rn(hi, lo); }
   __device__ __forceinline__ float minus(float y) const { return __fadd_rn(__fsub_rn(hi, y), lo); }
 };
@@ -58,6 +59,7 @@ __device__ __forceinline__ LogP log_prob(float a, float ae, float s, float mean,
   const float el = __fadd_rn(__fmaf_rn((float)e, kLn2Lo, __fadd_rn(logf(f), fix)), __fsub_rn(s, s));
   o.logs = __fadd_rn(eh, el);
   o.H = __fsub_rn(o.logs, mean);
+  o.never = false;
   o.hi = __fsub_rn(a, eh);
   const float b = __fsub_rn(o.hi, a);
   const float he = __fsub_rn(__fsub_rn(a, __fsub_rn(o.hi, b)), __fadd_rn(eh, b));
@@ -71,7 +73,9 @@ __device__ __forceinline__ LogP log_prob(const Args& A, float xa, const Part& P)
   const float a = __fmul_rn(d, A.inv_t);
   const float ae = __fmaf_rn(d, A.inv_t_lo, __fmaf_rn(d, A.inv_t, -a));
   // the largest term is exact
-  return log_prob(a, __fmaf_rn(kEx2Short, rcp(P.s), ae), P.s, __fmul_rn(mean, A.inv_t), mean, A.dk);
+  LogP o = log_prob(a, __fmaf_rn(kEx2Short, rcp(P.s), ae), P.s, __fmul_rn(mean, A.inv_t), mean, A.dk);
+  o.never = xa == -inf();
+  return o;
 }
 
 // What a row's terms need besides the sums.
@@ -115,9 +119,11 @@ __device__ __forceinline__ RowOut token_terms(const TokenArgs& A, const RowIn& i
   if (A.logp_ref) {
     const float d = -l.minus(in.ref);
     const float em = expm1f(d);
-    terms[1] = __fmaf_rn(w, __fsub_rn(em, d), terms[1]);
+    terms[1] = __fmaf_rn(w, em < inf() ? __fsub_rn(em, d) : em, terms[1]);  // both infinite where lp is -inf
     if (A.c_kl != 0.0f) c = __fmaf_rn(-A.c_kl, em, c);  // em may be beyond fp32
   }
+  // c would come to a logit of -inf, whose gradient is 0: L has none there, unless it does not move with lp
+  if (l.never && c != 0.0f) c = nan();
   terms[2] = __fmaf_rn(w, o.H, terms[2]);
   o.c = __fmul_rn(__fmul_rn(c, w), it);
   o.u = __fmul_rn(__fmul_rn(w, A.c_entropy), it);
@@ -503,7 +509,9 @@ __device__ __forceinline__ LogP log_prob(const Args& A, float xa, const Stream& 
   ae = __fmaf_rn(l, kLn2, __fmaf_rn(h, kLn2Rest, ae));
   ae = __fmaf_rn(-A.dk, xa, ae);  // x k has k's rounding in it too
   const float mean = __fdiv_rn(v.t, v.s);
-  return log_prob(a, fabsf(a) < inf() ? ae : 0.0f, v.s, __fmul_rn(mean, kLn2), __fdiv_rn(__fadd_rn(mean, v.c), A.k), A.dk);
+  LogP o = log_prob(a, fabsf(a) < inf() ? ae : 0.0f, v.s, __fmul_rn(mean, kLn2), __fdiv_rn(__fadd_rn(mean, v.c), A.k), A.dk);
+  o.never = xa == -inf();
+  return o;
 }
 
 // Whether a row's streamed sums hold: not for rows of nothing but -inf or values beyond 1e30 either way,
@@ -713,8 +721,6 @@ __global__ void __launch_bounds__(kStatThreads) k_token_stats(TokenArgs A, int p
   }
 }
 
-// Preference loss, first pass: log pi(token) - logp_ref and the softmax's statistics of every row
-// that counts (rows outside all sequences are masked rows).
 __device__ __forceinline__ int64_t clamp_row(int64_t v, int64_t n) { return v < 0 ? 0 : v > n ? n : v; }
 
 // The sequence that holds row i, or -1: the last q with seq_start[q] <= i, if i is before its end.
@@ -739,7 +745,8 @@ __global__ void __launch_bounds__(256) k_pref_index(PrefArgs A) {
 // The preference loss reads the logits twice: every row's coefficient waits for all rows of its pair.
 // First pass: the log ratio and the sums of every row that counts, streamed as in the token loss.  32 pairs
 // of 32,768 bf16 logits: two passes at 4.9 and 5.6 TB/s (62 % and 83 % of the DRAM's cycles).
-// row_is < 0 marks a row whose row_c is its maximum (see stream_holds) instead of the sums' reference.
+// row_is < 0 marks a row whose row_c is its maximum (see stream_holds) instead of the sums' reference, 0 one whose
+// token's logit is -inf: its gradient is NaN (as in the token loss), or zeros where its coefficient is 0.
 template <class T, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT) k_pref_rows(PrefArgs A) {
   __shared__ float sh[2][2][3 * NT / 32];
@@ -767,7 +774,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_pref_rows(PrefArgs A) {
       const LogP l = holds ? log_prob(A, xa, v) : log_prob(A, xa, p);
       A.row_d[i] = A.logp_ref ? l.minus(ref) : l.value();
       A.row_c[i] = holds ? v.c : p.m;
-      A.row_is[i] = holds ? __fdiv_rn(1.0f, v.s) : __fdiv_rn(-1.0f, p.s);
+      A.row_is[i] = l.never ? 0.0f : holds ? __fdiv_rn(1.0f, v.s) : __fdiv_rn(-1.0f, p.s);
     }
   }
 }
@@ -844,7 +851,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_pref_grad(PrefArgs A) {
     const int64_t a = A.token[i];
     const bool in = a >= 0 && a < A.V;
     float co = (q & 1) ? -A.coef[q >> 1] : A.coef[q >> 1];
-    if (!in) co = nan();
+    if (is == 0.0f && co == 0.0f) {
+      zero_row<T, NT>(g, V);
+      continue;
+    }
+    if (!in || is == 0.0f) co = nan();
     if (is > 0.0f) {
       stream_grad<T, NT, false>(x, g, V, A.k, c, 0.0f, __fmul_rn(-co, is), in ? (int)a : -1, co);
     } else {

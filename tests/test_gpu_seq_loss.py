@@ -510,3 +510,54 @@ def test_preference_pairs_without_weight_count_for_nothing(simx, V):
     assert not grad[:8].any() and np.isnan(margin[0]) and np.isnan(ratio[:2]).all()
     _close(grad[8:], ref["grad"][8:], ref["scale"][8:])
     _close(stats, ref["stats"], ref["stats_scale"])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [50, 300, 700, 5000, 40000, 70000])
+def test_token_of_probability_zero(simx, V, dtype):
+    """Actions whose logit is -inf: a ratio of 0 to an old policy takes nothing, on-policy and under a KL term
+    the loss has no gradient there; no logit of -inf ever gets a finite one but 0."""
+    rng = np.random.default_rng(V)
+    x = rng.standard_normal((4, V))
+    x[:, 3::5] = -np.inf
+    action, adv = np.array([3, 3, 3, 0]), np.array([1.0, -1.0, 0.0, 0.5])
+    par = dict(clip_low=0.2, clip_high=0.3, c_entropy=0.1)
+    old = np.full(4, -2.0)
+    exact, grad, stats, lp, H = _token(simx, x, action, dtype=dtype, adv=_dev(adv), logp_old=_dev(old), **par)
+    fine = seq.token_loss(exact[3:], action[3:], adv[3:], old[3:], weight=np.full(1, 0.25), **par)
+    rest = seq.token_loss(exact[:3], np.zeros(3, int), weight=np.full(3, 0.25), **par)  # their entropy alone
+    assert np.isneginf(lp[:3]).all()
+    _close(H[:3], rest["entropy"], 1 + rest["entropy"])
+    _close(grad, np.concatenate([rest["grad"], fine["grad"]]), np.concatenate([rest["scale"], fine["scale"]]), dtype)
+    assert not grad[:, 3::5].any()
+    # min(0, 0.8) for the first, -0.8 clipped for the second
+    _close(stats[1], fine["stats"][1] + 0.25 * 0.8, fine["stats_scale"][1] + 0.25)
+    _close(stats[4], fine["stats"][4] + 0.25, fine["stats_scale"][4] + 0.25)
+    _, grad, stats, _, _ = _token(simx, x, action, dtype=dtype, adv=_dev(adv), **par)
+    fine = seq.token_loss(exact[3:], action[3:], adv[3:], weight=np.full(1, 0.25), **par)
+    assert np.isnan(grad[:2]).all() and abs(stats[1] + 0.125) <= TOL
+    _close(grad[2:], np.concatenate([rest["grad"][2:], fine["grad"]]), np.concatenate([rest["scale"][2:], fine["scale"]]), dtype)
+    for c_kl in (0.0, 0.1):
+        _, grad, stats, _, _ = _token(simx, x, action, dtype=dtype, adv=_dev(adv), logp_old=_dev(old), logp_ref=_dev(old),
+                                      c_kl=c_kl, **par)
+        assert np.isposinf(stats[2]) and np.isfinite(grad[3]).all()
+        assert np.isnan(grad[:3]).all() if c_kl else np.isfinite(grad).all()
+        assert np.isposinf(stats[0]) if c_kl else np.isfinite(stats[0])
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("V", [60, 5000, 70000])
+def test_preference_token_of_probability_zero(simx, V, inplace):
+    """In a preferred sequence the loss is infinite and only that row has no gradient; in the other one the pair is
+    settled and takes nothing."""
+    x, token, start, kw = _pref_case([3, 2, 2, 3], V, 7, "f32")
+    kw["mask"][:] = 1
+    x[1, token[1]] = x[8, token[8]] = -np.inf
+    grad, stats, ratio, margin = _pref(simx, x, token, start, kw, dict(beta=0.2), "f32", inplace=inplace)
+    assert np.isneginf(ratio[[0, 3]]).all() and np.isneginf(margin[0]) and np.isposinf(margin[1])
+    assert np.isposinf(stats[0]) and np.isnan(grad[1]).all() and not grad[5:].any()
+    c = -kw["weight"][0] * np.float64(np.float32(0.2))
+    for i in (0, 2, 3, 4):
+        p = np.exp(seq.log_softmax(x[i:i + 1])[0])
+        hot = np.arange(V) == token[i]
+        _close(grad[i], (c if i < 3 else -c) * (hot - p), abs(c) * (hot + p))
