@@ -577,7 +577,9 @@ typedef struct simx_seq {
  * dropped).  It is evaluated as s_t + (1 - a_t)(x_t - s_t), which keeps long memories exact; a state
  * that is not finite becomes NaN.  h_last [batch][channels] = the state that the next call continues from (h0 there):
  * done_{len-1} ? 0 : h_{len-1}, and h0 for len == 0; it is the unrounded state, and it may be h0's own
- * buffer.  len == 1 is the single-token step of serving.  bias [channels], h0, h_last, done, dh_last,
+ * buffer.  Long sequences are shared by blocks that wait for each other's parts, about a second each at
+ * most; past that the states (backward: the lambdas) that come from other blocks are NaN, and with them
+ * all that depends on them.  len == 1 is the single-token step of serving.  bias [channels], h0, h_last, done, dh_last,
  * dbias and dh0 may be NULL.  An empty problem (batch or channels 0) touches nothing.
  *
  * simx_gated_scan_grad: given dh (the gradient of h as an output) and dh_last (of h_last; NULL:

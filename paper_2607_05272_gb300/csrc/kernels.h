@@ -94,8 +94,8 @@ template <class K>
 inline cudaError_t allow_smem(K* kernel, int most) {
   return cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
 }
-// Weight copies withheld at the end of each block's sequence (SIMX_WITHHOLD_COPIES, 0 without it): a
-// wait that nothing ends, for the tests of what a call reports when a bounded wait runs out.
+// Weight copies withheld at the end of each block's sequence, and the posts of each cluster's last block in
+// the gated scan (SIMX_WITHHOLD_COPIES, 0 without it): a wait that nothing ends, for the tests of what a call reports when a bounded wait runs out.
 inline uint32_t copies_withheld() {
   const char* v = getenv("SIMX_WITHHOLD_COPIES");
   return v ? (uint32_t)atoi(v) : 0u;

@@ -23,6 +23,7 @@
 #include <initializer_list>
 
 #include "kernels.h"
+#include "peer_round.h"
 #include "seq_common.cuh"
 
 namespace simx {
@@ -641,7 +642,7 @@ struct WideAhead {
 template <int NW, int CLT>
 struct WideShared {
   float4 a[2 * NW * kWidePitch / 4], b[2 * NW * kWidePitch / 4];  // [group][channel]; a also takes the states
-  float2 peer[2][CLT][kWideChannels];                             // [parity][rank]: {A, B}
+  float2 peer[2][CLT][kWideChannels];                             // [slot][rank]: {A, B}
   uint64_t bar[2];
 };
 
@@ -657,7 +658,7 @@ struct Joiner {
 // return s is the state before the thread's first step, and carry that after the round.
 template <int NW, int CLT, bool FORGET>
 __device__ __forceinline__ void wide_states(const float (&A)[4], const float (&B)[4], float& carry, float (&s)[4],
-                                            uint32_t rank, uint32_t turn, bool& lost, WideShared<NW, CLT>& sh) {
+                                            uint32_t rank, PeerRound& peers, WideShared<NW, CLT>& sh) {
   const Joiner<NW> J;
   constexpr int TPC = Joiner<NW>::TPC;
   const int group = (int)threadIdx.x / kWideLanes, cl = (int)threadIdx.x % kWideLanes;
@@ -693,20 +694,20 @@ __device__ __forceinline__ void wide_states(const float (&A)[4], const float (&B
   if (CLT == 1) {
     carry = apply<FORGET>(ja, jb, carry);
   } else {
-    // A block may post a round while another still reads the one before, but not the one after: that takes
-    // the other's post of this round.
-    const int parity = (int)(turn & 1u);
-    uint64_t* bar = &sh.bar[parity];
-    if (threadIdx.x == 0) tcx::mbar_arrive_expect_tx(bar, (uint32_t)(8 * kWideChannels * CLT));
-    for (int r = J.q; r < CLT; r += TPC) post_peer(&sh.peer[parity][rank][J.ch], bar, (uint32_t)r, make_float2(ja, jb));
-    lost = lost || !tcx::mbar_wait(bar, (turn >> 1) & 1u, kPeerCycles);
+    const uint32_t slot = peers.slot();
+    uint64_t* bar = &sh.bar[slot];
+    if (peers.posts()) {
+      if (threadIdx.x == 0) tcx::mbar_arrive_expect_tx(bar, (uint32_t)(8 * kWideChannels * CLT));
+      for (int r = J.q; r < CLT; r += TPC) post_peer(&sh.peer[slot][rank][J.ch], bar, (uint32_t)r, make_float2(ja, jb));
+    }
+    peers.end(!peers.lost() && tcx::mbar_wait(bar, peers.parity(), kPeerCycles));
 #pragma unroll
     for (int r = 0; r < CLT; ++r) {
-      const float2 m = sh.peer[parity][r][J.ch];
+      const float2 m = sh.peer[slot][r][J.ch];
       if (r == (int)rank) in = carry;
       carry = apply<FORGET>(m.x, m.y, carry);
     }
-    if (lost) in = carry = nan();  // a post that never came: what the cluster still computes is NaN
+    if (peers.lost()) in = carry = nan();  // a post that never came: the states that come to this block are NaN from here on
   }
   float v = J.q == 0 ? in : apply<FORGET>(pa, pb, in);
 #pragma unroll
@@ -736,7 +737,7 @@ __device__ __forceinline__ uint32_t group_bits(uint8_t byte) {
 }
 
 template <class T, bool DONE, int CLT, int ACCESS>
-__global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles) {
+__global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles, bool withheld) {
   constexpr int S = kTileSteps, NW = 8, TB = 2 * NW * S;
   constexpr int64_t step = (int64_t)CLT * TB;
   extern __shared__ uint4 slots[];
@@ -749,8 +750,7 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
   const int64_t rounds = (A.len + step - 1) / step;
   WideAhead<T, 2, S, ACCESS> in;
   in.start(slots);
-  uint32_t turn = 0;
-  bool lost = false;
+  PeerRound peers{withheld && rank == CLT - 1 ? 4u : 0u};  // withheld: the last block's posts are never made (tests)
   for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
     const int64_t b = tile / per, c0 = (tile - b * per) * kWideChannels, c = c0 + 4 * cl;
     const bool mine = c < A.channels, joins = c0 + J.ch < A.channels;
@@ -809,7 +809,7 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
         }
         if (DONE && resets) a[i] = kForget;
       }
-      wide_states<NW, CLT, DONE>(a, s, carry, st, rank, turn++, lost, sh);
+      wide_states<NW, CLT, DONE>(a, s, carry, st, rank, peers, sh);
       T* p = h;
 #pragma unroll
       for (int k = 0; k < S; ++k, p += A.h.st) {
@@ -830,7 +830,7 @@ __global__ void __launch_bounds__(256, 2) k_scan_wide(simx_scan A, int64_t tiles
 
 // Backward, on the steps in reverse order; part [batch * CLT][channels]: sums of dgate (or null).
 template <class T, bool DONE, int CLT, int ACCESS>
-__global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t tiles, float* part) {
+__global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t tiles, float* part, bool withheld) {
   constexpr int S = kTileSteps, NW = 4, TB = 2 * NW * S;
   constexpr int64_t step = (int64_t)CLT * TB;
   extern __shared__ uint4 slots[];
@@ -844,8 +844,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
   const int64_t rounds = (A.len + step - 1) / step;
   WideAhead<T, 4, S, ACCESS> in;
   in.start(slots);
-  uint32_t turn = 0;
-  bool lost = false;
+  PeerRound peers{withheld && rank == CLT - 1 ? 4u : 0u};  // withheld: the last block's posts are never made (tests)
   for (int64_t tile = blockIdx.x / CLT; tile < tiles; tile += gridDim.x / CLT) {
     const int64_t b = tile / per, c0 = (tile - b * per) * kWideChannels, c = c0 + 4 * cl;
     const bool mine = c < A.channels, joins = c0 + J.ch < A.channels;
@@ -924,7 +923,7 @@ __global__ void __launch_bounds__(128, 3) k_scan_grad_wide(simx_scan A, int64_t 
         }
         if (DONE && own) a[i] = kForget;
       }
-      wide_states<NW, CLT, DONE>(a, m, carry, mu, rank, turn++, lost, sh);
+      wide_states<NW, CLT, DONE>(a, m, carry, mu, rank, peers, sh);
       T* px = dx;
       T* pg = dgate;
 #pragma unroll
@@ -1062,13 +1061,14 @@ cudaError_t launch_tiles(K* kernel, const ScanPlan& p, int threads, size_t smem,
 template <class T, bool DONE, int ACCESS>
 cudaError_t scan_tiles(const simx_scan& a, const ScanPlan& p, cudaStream_t s) {
   if (p.wide) {
+    const bool withheld = p.cluster > 1 && copies_withheld() != 0u;
     const int th = 32 * kFwdWarps;
     const size_t smem = (size_t)th * 2 * kTileSteps * 4 * sizeof(T);
-    if (p.cluster == 8) return launch_tiles(k_scan_wide<T, DONE, 8, ACCESS>, p, th, smem, s, a, p.tiles);
-    if (p.cluster == 4) return launch_tiles(k_scan_wide<T, DONE, 4, ACCESS>, p, th, smem, s, a, p.tiles);
+    if (p.cluster == 8) return launch_tiles(k_scan_wide<T, DONE, 8, ACCESS>, p, th, smem, s, a, p.tiles, withheld);
+    if (p.cluster == 4) return launch_tiles(k_scan_wide<T, DONE, 4, ACCESS>, p, th, smem, s, a, p.tiles, withheld);
     if constexpr (ACCESS == WHOLE) {
-      if (p.cluster == 2) return launch_tiles(k_scan_wide<T, DONE, 2, WHOLE>, p, th, smem, s, a, p.tiles);
-      return launch_tiles(k_scan_wide<T, DONE, 1, WHOLE>, p, th, smem, s, a, p.tiles);
+      if (p.cluster == 2) return launch_tiles(k_scan_wide<T, DONE, 2, WHOLE>, p, th, smem, s, a, p.tiles, withheld);
+      return launch_tiles(k_scan_wide<T, DONE, 1, WHOLE>, p, th, smem, s, a, p.tiles, false);
     }
   }
   constexpr int VEC = ACCESS == WHOLE ? 4 : 1;
@@ -1078,13 +1078,14 @@ cudaError_t scan_tiles(const simx_scan& a, const ScanPlan& p, cudaStream_t s) {
 template <class T, bool DONE, int ACCESS>
 cudaError_t scan_grad_tiles(const simx_scan& a, const ScanPlan& p, float* part, cudaStream_t s) {
   if (p.wide) {
+    const bool withheld = p.cluster > 1 && copies_withheld() != 0u;
     const int th = 32 * kGradWarps;
     const size_t smem = (size_t)th * 4 * kTileSteps * 4 * sizeof(T);
-    if (p.cluster == 8) return launch_tiles(k_scan_grad_wide<T, DONE, 8, ACCESS>, p, th, smem, s, a, p.tiles, part);
-    if (p.cluster == 4) return launch_tiles(k_scan_grad_wide<T, DONE, 4, ACCESS>, p, th, smem, s, a, p.tiles, part);
+    if (p.cluster == 8) return launch_tiles(k_scan_grad_wide<T, DONE, 8, ACCESS>, p, th, smem, s, a, p.tiles, part, withheld);
+    if (p.cluster == 4) return launch_tiles(k_scan_grad_wide<T, DONE, 4, ACCESS>, p, th, smem, s, a, p.tiles, part, withheld);
     if constexpr (ACCESS == WHOLE) {
-      if (p.cluster == 2) return launch_tiles(k_scan_grad_wide<T, DONE, 2, WHOLE>, p, th, smem, s, a, p.tiles, part);
-      return launch_tiles(k_scan_grad_wide<T, DONE, 1, WHOLE>, p, th, smem, s, a, p.tiles, part);
+      if (p.cluster == 2) return launch_tiles(k_scan_grad_wide<T, DONE, 2, WHOLE>, p, th, smem, s, a, p.tiles, part, withheld);
+      return launch_tiles(k_scan_grad_wide<T, DONE, 1, WHOLE>, p, th, smem, s, a, p.tiles, part, false);
     }
   }
   constexpr int VEC = ACCESS == WHOLE ? 4 : 1;

@@ -343,3 +343,36 @@ def test_clusters_with_the_state_in_place_and_ends_everywhere(simx):
         simx.gated_scan(x, gate, h, h0=state, done=dn, h_last=state)
         torch.cuda.synchronize()
         assert torch.equal(state, last)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [64, 66, 67])
+def test_clusters_say_nan_where_a_post_never_comes(simx, C, dtype, monkeypatch):
+    """SIMX_WITHHOLD_COPIES keeps the last block of each cluster from posting, so the bounded waits (about a second)
+    run out: what depends on a state from another block is NaN, the rest is what it was."""
+    T = 5000
+    c = _case(1, T, C, 41, 0.004)
+    c["done"][0, :8] = c["done"][0, -8:] = 0
+    x, gate, dh = (_tensor((1, T, C), dtype, "batch", c[k]) for k in ("x", "gate", "dh"))
+    dn, h0 = _done(c["done"], "batch"), _dev(c["h0"])
+    ws = torch.empty(simx.gated_scan_workspace_size(1, T, C), dtype=torch.uint8, device="cuda")
+
+    def call(saved=None):
+        h, dx, dg = (_tensor((1, T, C), dtype, "batch") for _ in range(3))
+        last, d0, db = torch.zeros((1, C), device="cuda"), torch.zeros((1, C), device="cuda"), torch.zeros(C, device="cuda")
+        simx.gated_scan(x, gate, h, h0=h0, done=dn, h_last=last)
+        simx.gated_scan_grad(x, gate, h if saved is None else saved, dh, dx, dg, ws, h0=h0, done=dn, dbias=db, dh0=d0)
+        torch.cuda.synchronize()
+        return h, dx, dg, last, d0, db
+
+    good = call()
+    monkeypatch.setenv("SIMX_WITHHOLD_COPIES", "1")
+    bad = call(good[0])
+    monkeypatch.delenv("SIMX_WITHHOLD_COPIES")
+    assert all(torch.equal(a, b) for a, b in zip(good, call()))
+    h, dx, dg, last, d0, db = bad
+    assert torch.isnan(h[:, 0]).all() and torch.isnan(dx[:, -1]).all() and torch.isnan(dg[:, -1]).all()
+    assert torch.isnan(last).all() and torch.isnan(d0).all() and torch.isnan(db).all()
+    for a, b in zip(good[:3], bad[:3]):
+        there = ~torch.isnan(b)
+        assert there.any() and torch.equal(a[there], b[there])
