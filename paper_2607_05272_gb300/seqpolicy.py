@@ -12,9 +12,11 @@ episode: per decision
 Rollouts take the single-token forms, the state updated in place; updates take whole time-major
 buffers [H][E], as ``rollout_collect`` lays them out.  ``update`` is one step of the clipped policy
 loss with a KL term to the policy that collected the rollout; ``preference_update`` is one step of the
-preference loss on pairs of envs, the one with the larger return preferred.  Every nonlinear step, both
-losses, all their gradients and Adam run in the library's kernels; the matrix products between them are
-``torch.matmul``.
+preference loss on pairs of envs, the one with the larger return preferred.  Actions are sampled without
+dropout and every update draws a mask of its own, so it evaluates the parameters that collected the
+rollout under that mask too: ratios, KL terms and margins compare parameters, not masks.  Every nonlinear
+step, both losses, all their gradients and Adam run in the library's kernels; the matrix products between
+them are ``torch.matmul``.
 
 Command line: ``python -m paper_2607_05272_gb300.seqpolicy --workload c3s --iters 80``.
 """
@@ -61,7 +63,7 @@ class SeqPolicy:
         self.m, self.v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
         self.t = torch.zeros(1, dtype=torch.int64, device="cuda")
         self.gen = gen
-        self.calls = 0  # training passes so far: the dropout's step
+        self.calls = 0  # updates so far: the dropout's step
 
         def ws(size):
             return torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
@@ -89,10 +91,15 @@ class SeqPolicy:
         simx.dropout_add_norm(o, w["gain2"], y2, residual=z1)
         return y2 @ w["w_h"].t()
 
-    def forward(self, obs, done, state, p: float, step: int) -> dict:
+    def views(self, flat) -> dict:
+        """The parameters by name in a vector laid out as `flat`."""
+        return {k: flat[v.storage_offset():v.storage_offset() + v.numel()].view(v.shape) for k, v in self.w.items()}
+
+    def forward(self, obs, done, state, p: float, step: int, w=None) -> dict:
         """The pass over a rollout: obs [H, E, D], done [H, E], state [E, C] before its first
-        decision.  Returns what the backward pass takes, logits [H * E, A] among it."""
-        w, c, (hh, e, d) = self.w, self.C, obs.shape
+        decision; w: other parameters than the policy's own.  Returns what the backward pass takes,
+        logits [H * E, A] among it."""
+        w, c, (hh, e, d) = w or self.w, self.C, obs.shape
         n = hh * e
         f = dict(obs=obs.reshape(n, d), done=done.t(), state=state, p=p, step=step, shape=(hh, e))
 
@@ -144,12 +151,14 @@ class SeqPolicy:
     # ------------------------------------------------------------------ rollouts and updates
 
     def rollout(self, sim, state) -> dict:
-        """H decisions of every env, sampled; the state goes on in place."""
+        """H decisions of every env, sampled; the state goes on in place.  b["params"]: the parameters that
+        sampled them."""
         hh, e = self.H, self.E
         b = dict(obs=torch.empty((hh, e, self.D), device="cuda"),
                  action=torch.empty((hh, e), dtype=torch.int64, device="cuda"),
                  logp=torch.empty((hh, e), device="cuda"), reward=torch.empty((hh, e), device="cuda"),
-                 done=torch.empty((hh, e), dtype=torch.uint8, device="cuda"), state=state.clone())
+                 done=torch.empty((hh, e), dtype=torch.uint8, device="cuda"), state=state.clone(),
+                 params=self.flat.clone())
         cols = torch.empty((self.D, e), device="cuda")
         sim.observe(cols)
         for t in range(hh):
@@ -164,6 +173,17 @@ class SeqPolicy:
             state.masked_fill_(b["done"][t, :, None] != 0, 0.0)
         return b
 
+    def reference(self, b: dict, step: int):
+        """Log probabilities [H, E] of a rollout's actions by the parameters that collected it, under the
+        dropout mask of `step`; b["logp"] as it is where no dropout or no parameters are there."""
+        if "params" not in b or self.p == 0.0:
+            return b["logp"]
+        f = self.forward(b["obs"], b["done"], b["state"], self.p, step, self.views(b["params"]))
+        logp = torch.empty_like(b["logp"])
+        simx.token_loss_grad(f["logits"], b["action"].view(-1), None, self.stats, self.loss_ws,
+                             logp=logp.view(-1))
+        return logp
+
     def _adam(self, lr):
         simx.adam_step(self.flat, self.grad_flat, self.m, self.v, self.t, lr, max_grad_norm=0.5,
                        workspace=self.adam_ws)
@@ -172,9 +192,9 @@ class SeqPolicy:
                c_entropy: float = 0.01):
         """One step of the clipped policy loss on a rollout with advantages [H, E]; the KL term is to
         the policy that collected it.  Returns the loss's statistics (device)."""
+        logp = self.reference(b, self.calls).view(-1)
         f = self.forward(b["obs"], b["done"], b["state"], self.p, self.calls)
         self.calls += 1
-        logp = b["logp"].view(-1)
         simx.token_loss_grad(f["logits"], b["action"].view(-1), adv.reshape(-1), self.stats,
                              self.loss_ws, logp_old=logp, logp_ref=logp, clip_low=clip,
                              clip_high=clip, c_kl=c_kl, c_entropy=c_entropy, grad=f["logits"])
@@ -191,6 +211,7 @@ class SeqPolicy:
         swap = (ret[:, 1] > ret[:, 0]).long()[:, None]
         pair = torch.arange(e, device="cuda").view(-1, 2)
         order = torch.cat([pair.gather(1, swap), pair.gather(1, 1 - swap)], 1).view(-1)
+        logp = self.reference(b, self.calls)
         f = self.forward(b["obs"], b["done"], b["state"], self.p, self.calls)
         self.calls += 1
 
@@ -199,7 +220,7 @@ class SeqPolicy:
         logits = rows(f["logits"].view(hh, self.E, self.A))
         start = torch.arange(e + 1, device="cuda") * hh
         simx.preference_loss_grad(logits, rows(b["action"]), start, self.pref_stats, self.pref_ws,
-                                  logp_ref=rows(b["logp"]), beta=beta, grad=logits)
+                                  logp_ref=rows(logp), beta=beta, grad=logits)
         dlogits = torch.zeros((self.E, hh, self.A), device="cuda")
         dlogits[order] = logits.view(e, hh, self.A)
         self.backward(f, dlogits.transpose(0, 1).reshape(hh * self.E, self.A))

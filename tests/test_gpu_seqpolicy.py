@@ -126,3 +126,26 @@ def test_training_run_learns_and_repeats(sp):
     frozen = sp.train(lr=0.0, preferences=0, **kw)
     tail = lambda r: np.mean([h["mean_reward"] for h in r[-10:]])  # noqa: E731
     assert tail(runs[0]) > tail(frozen) + 0.5
+
+
+def test_an_unchanged_policy_is_its_own_reference(sp, monkeypatch):
+    """Before any step of the optimiser every ratio is 1 and the KL and all margins are 0, dropout or not, in every
+    epoch.  log probabilities of one network and mask, within 1e-6 (1 + |lp|) of each other (|lp| < 10 here): a KL
+    of d^2 / 2, margins of 0.1 times 32 such differences."""
+    e, hh = 64, 16
+    sim = sp.simx.Sim(sp.W.CONFIGS["c3s"](e))
+    sim.reset(3)
+    dims, has_value = sp.W.mlp_dims("c3s")
+    pol = sp.SeqPolicy(sim.D, dims[-1] - int(has_value), e, hh, 64, p=0.3, seed=2)
+    _frozen(pol, monkeypatch)
+    state = torch.zeros((e, pol.C), device="cuda")
+    for _ in range(2):
+        b = pol.rollout(sim, state)
+        adv = torch.randn((hh, e), device="cuda")
+        for _ in range(2):
+            s = pol.update(b, adv, c_entropy=0.0).tolist()
+            assert abs(s[2]) <= 1e-9 and s[4] == 0.0
+            assert abs(s[1] + adv.mean().item()) <= 2e-5 * adv.abs().mean().item()
+        q = pol.preference_update(b).tolist()
+        assert abs(q[0] - np.log(2)) <= 1e-4 and abs(q[2]) <= 1e-4
+    sim.close()
