@@ -204,11 +204,12 @@ class SeqPolicy:
 
     def preference_update(self, b: dict, lr: float = 1e-4, beta: float = 0.1):
         """One step of the preference loss on pairs of envs (2p, 2p + 1): the sequence of the larger
-        return is preferred, the rollout's log probabilities are the reference.  Returns the loss's
-        statistics (device)."""
+        return is preferred (equal returns: neither, the pair counts for nothing), the rollout's log
+        probabilities are the reference.  Returns the loss's statistics (device)."""
         hh, e = self.H, self.E // 2 * 2
         ret = b["reward"].sum(0)[:e].view(-1, 2)
         swap = (ret[:, 1] > ret[:, 0]).long()[:, None]
+        weight = (ret[:, 1] != ret[:, 0]).float() / max(len(ret), 1)
         pair = torch.arange(e, device="cuda").view(-1, 2)
         order = torch.cat([pair.gather(1, swap), pair.gather(1, 1 - swap)], 1).view(-1)
         logp = self.reference(b, self.calls)
@@ -220,7 +221,7 @@ class SeqPolicy:
         logits = rows(f["logits"].view(hh, self.E, self.A))
         start = torch.arange(e + 1, device="cuda") * hh
         simx.preference_loss_grad(logits, rows(b["action"]), start, self.pref_stats, self.pref_ws,
-                                  logp_ref=rows(logp), beta=beta, grad=logits)
+                                  logp_ref=rows(logp), weight=weight, beta=beta, grad=logits)
         dlogits = torch.zeros((self.E, hh, self.A), device="cuda")
         dlogits[order] = logits.view(e, hh, self.A)
         self.backward(f, dlogits.transpose(0, 1).reshape(hh * self.E, self.A))

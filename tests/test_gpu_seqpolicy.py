@@ -149,3 +149,21 @@ def test_an_unchanged_policy_is_its_own_reference(sp, monkeypatch):
         q = pol.preference_update(b).tolist()
         assert abs(q[0] - np.log(2)) <= 1e-4 and abs(q[2]) <= 1e-4
     sim.close()
+
+
+def test_envs_of_equal_return_prefer_neither(sp, monkeypatch):
+    """The first pair's returns are equal: loss and gradient are the other pairs' alone, whichever env comes first."""
+    hh, e = 12, 6
+    pol = sp.SeqPolicy(5, 7, e, hh, 32, p=0.1, seed=6)
+    _frozen(pol, monkeypatch)
+    b = _batch(pol, hh, e, 4)
+    b["reward"][:, 0] = b["reward"][:, 1]
+    out = []
+    for logp in (-2.0, -1.0):  # of the second env: the pair's margin, not the others'
+        b["logp"][:, 1] = logp
+        pol.calls = 0
+        out.append((pol.preference_update(b, beta=0.3).clone(), pol.grad_flat.clone()))
+    assert out[0][1].any() and all(torch.equal(x, y) for x, y in zip(*out))
+    b["reward"].zero_()
+    stats = pol.preference_update(b, beta=0.3)
+    assert not stats.any() and not pol.grad_flat.any()
