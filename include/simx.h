@@ -489,7 +489,8 @@ simx_status simx_adam_step(float* d_params, const float* d_grad, float* d_m, flo
 typedef enum simx_dtype { SIMX_F32 = 0, SIMX_BF16 = 1 } simx_dtype;
 
 /* n rows of logits over a vocabulary: row i at i * ld, its gradient at i * grad_ld (grad NULL: none
-   is computed; grad may be logits itself with grad_ld == ld).  pi = softmax(logits / temperature).
+   is computed; grad may be logits itself with grad_ld == ld).  pi = softmax(logits / temperature),
+   temperature positive and log2(e) / temperature within fp32.
    1 <= vocab < 2^31 - 2^16.  A logit of -inf has probability 0 and gradient 0; a row that has a NaN,
    +inf, or nothing above -inf gives NaN in its outputs, and so does a token outside the vocabulary.
    Where the token's own logit is -inf, its log probability is -inf and the values are what the

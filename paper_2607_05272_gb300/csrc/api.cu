@@ -932,13 +932,16 @@ static simx_status check_aligned(std::initializer_list<const void*> all, int byt
   return low & (uintptr_t)(bytes - 1) ? fail(SIMX_EINVAL, "a pointer to %d-byte elements is misaligned", bytes) : SIMX_OK;
 }
 
+static const double kLog2e64 = 1.44269504088896340736;
+
 static simx_status check_logits(const simx_logits* x) {
   if (!x) return fail(SIMX_EINVAL, "logits are NULL");
   const int es = elem_bytes(x->dtype);
   if (!es) return fail(SIMX_EINVAL, "dtype %d", x->dtype);
   if (x->n < 0 || x->n > kMaxRows) return fail(SIMX_EINVAL, "%lld rows", (long long)x->n);
   if (x->vocab < 1 || x->vocab >= ((int64_t)1 << 31) - 65536) return fail(SIMX_EINVAL, "vocab %lld", (long long)x->vocab);
-  if (!(x->temperature > 0.0f) || !std::isfinite(x->temperature) || !std::isfinite((float)(1.0 / x->temperature)))
+  // the kernels scale by log2(e) / temperature
+  if (!(x->temperature > 0.0f) || !std::isfinite(x->temperature) || !std::isfinite((float)(kLog2e64 / x->temperature)))
     return fail(SIMX_EINVAL, "temperature %g", (double)x->temperature);
   if (x->n == 0) return SIMX_OK;
   if (!x->logits) return fail(SIMX_EINVAL, "logits are NULL");
@@ -974,9 +977,9 @@ simx_status simx_token_loss_grad(const simx_logits* x, const simx_token_loss* l,
   a.V = x->vocab;
   a.dtype = x->dtype;
   a.inv_t = (float)(1.0 / x->temperature);
-  a.k = (float)(1.44269504088896340736 / x->temperature);
+  a.k = (float)(kLog2e64 / x->temperature);
   a.inv_t_lo = (float)(1.0 / x->temperature - (double)a.inv_t);
-  a.dk = (float)((double)a.k / 1.44269504088896340736 - 1.0 / x->temperature);
+  a.dk = (float)((double)a.k / kLog2e64 - 1.0 / x->temperature);
   a.action = l->action;
   a.adv = l->adv;
   a.logp_old = l->logp_old;
@@ -1022,9 +1025,9 @@ simx_status simx_preference_loss_grad(const simx_logits* x, const simx_preferenc
   a.V = x->vocab;
   a.dtype = x->dtype;
   a.inv_t = (float)(1.0 / x->temperature);
-  a.k = (float)(1.44269504088896340736 / x->temperature);
+  a.k = (float)(kLog2e64 / x->temperature);
   a.inv_t_lo = (float)(1.0 / x->temperature - (double)a.inv_t);
-  a.dk = (float)((double)a.k / 1.44269504088896340736 - 1.0 / x->temperature);
+  a.dk = (float)((double)a.k / kLog2e64 - 1.0 / x->temperature);
   a.token = l->token;
   a.start = l->seq_start;
   a.mask = l->mask;

@@ -227,3 +227,13 @@ def test_packed_images_are_the_structures(image, cls):
         with pytest.raises(simx.SimxError) as e:
             image(*[bad] * n)
         assert e.value.status == simx.EINVAL
+
+
+@pytest.mark.parametrize("t", [3e-39, 3.5e-39, 4.2e-39])
+def test_temperatures_whose_scale_is_beyond_fp32(lib, t):
+    """1 / t is finite in fp32, log2(e) / t is not: equal logits would give 0 times infinity."""
+    a, b = _logits(temperature=t), _token()
+    assert a.temperature > 0 and 1 / a.temperature < 3.4028235e38 < 1.442695 / a.temperature
+    _refused(lib, lib.simx_token_loss_grad(C.byref(a), C.byref(b), FAKE, 1 << 30, None))
+    p = simx.PreferenceLoss(token=FAKE, seq_start=FAKE, pairs=2, beta=0.1, stats=FAKE)
+    _refused(lib, lib.simx_preference_loss_grad(C.byref(a), C.byref(p), FAKE, 1 << 30, None))
