@@ -1004,13 +1004,17 @@ ScanPlan plan_scan(int64_t batch, int64_t len, int64_t channels, int access, int
   const int64_t tiles = batch * up(channels, kWideChannels);
   // off alignment only large clusters are ever the better choice
   for (int cl = aligned ? 1 : 4; cl <= kMaxCluster && (cl == 1 || block * cl <= len); cl *= 2) {
+    // fp32 gradients in clusters of 8 fit two blocks to an SM: 64 KB of copies, 12.6 KB of tables and posts and the
+    // reserved kilobyte each, of 228 (48 x 8192 x 64: clusters of 4 126 us, of 8 136).  Off alignment the measured
+    // rounds below have that in them already (24 x 4096 x 66: clusters of 8 101, of 4 111).
+    const int64_t places = grad && dtype == SIMX_F32 && access == WHOLE && cl == 8 ? (int64_t)sm_count() * 2 : slots;
     // an SM with one block, and what the others add
     const double full = std::min(1.0, (double)(tiles * cl) / (double)slots);
     const double round = access == WHOLE ? (grad ? 3.5 : 2.5)
                          : access == WORDS ? (grad ? (dtype == SIMX_F32 ? 4.0 + 6.0 * full : 4.0 + 3.0 * full) : (dtype == SIMX_F32 ? 2.5 + 2.5 * full : 2.5 + 1.5 * full))
                                            : (grad ? 6.5 + 4.0 * full : 3.0 + 2.4 * full);
     const double posts = cl == 1 ? 1.0 : cl == 2 ? 1.03 : cl == 4 ? 1.1 : 1.25;
-    const double cost = (double)up(tiles * cl, slots) * (double)(up(len, block * cl) + 1) * round * posts;
+    const double cost = (double)up(tiles * cl, places) * (double)(up(len, block * cl) + 1) * round * posts;
     if (cost < best) {
       best = cost;
       p.wide = true;

@@ -376,3 +376,20 @@ def test_clusters_say_nan_where_a_post_never_comes(simx, C, dtype, monkeypatch):
     for a, b in zip(good[:3], bad[:3]):
         there = ~torch.isnan(b)
         assert there.any() and torch.equal(a[there], b[there])
+
+
+@pytest.mark.parametrize("dtype,B,cluster", [("f32", 48, 4), ("f32", 30, 8), ("bf16", 48, 8)])
+def test_clusters_by_the_blocks_that_fit(simx, dtype, B, cluster):
+    """One wave of blocks, where they fit: fp32 gradients in clusters of 8 two to an SM, the others three.  Every
+    block leaves a row of partial sums of dbias in the workspace."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    if sms != 152:
+        pytest.skip("sizes for 152 SMs")
+    T, C = 2048, 64
+    t = [_tensor((B, T, C), dtype, "batch", np.ones((B, T, C))) for _ in range(6)]
+    size = simx.gated_scan_workspace_size(B, T, C)
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    simx.gated_scan_grad(*t, ws, dbias=torch.empty(C, device="cuda"))
+    torch.cuda.synchronize()
+    written = ~torch.isnan(ws.view(torch.float32)).view(-1, C)
+    assert written[:B * cluster].all() and not written[B * cluster:].any()
