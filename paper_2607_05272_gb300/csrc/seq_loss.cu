@@ -8,9 +8,9 @@
 //   dL / dx_j = (c (delta_ja - p_j) + u p_j (log p_j + H)) / T.
 // Bound by HBM: a row is read once and its gradient written once; about 10 operations per logit.
 // Measured on one GB300 (floors at 6783 GB/s): token loss of 8192 x 131,072 bf16, an eighth of the rows
-// without weight, 742 us (594), 1021 x 50,001 fp32 76 (53), 8 x 131,072 bf16 8 and 8192 x 48 fp32 4.5 on the
+// without weight, 739 us (594), 1021 x 50,001 fp32 76 (53), 8 x 131,072 bf16 8 and 8192 x 48 fp32 4.5 on the
 // GPU, where a call's arguments take the host 13; preference loss of 32 pairs of up to 512 tokens over
-// 32,768 bf16 logits 469 (297, or 442 with the second read that its coefficients need).
+// 32,768 bf16 logits 467 (297, or 442 with the second read that its coefficients need).
 #include <algorithm>
 
 #include "kernels.h"
@@ -305,7 +305,7 @@ __device__ __noinline__ void row_grad_loop(const T* x, T* g, int V, const Args& 
 // e = 2^(x k - c) with an integer reference c of its own, raised when a logit passes it, so that sums move
 // to another reference by an exact power of two.  No block waits for another one, which is what a row in
 // a cluster's registers costs: it is the kernel of calls with enough rows to fill the GPU.  8192 rows of
-// 131,072 bf16 logits: 742 us, 5.4 TB/s of what the call cannot do without; DRAM moves 8 % more than that,
+// 131,072 bf16 logits: 739 us, 5.4 TB/s of what the call cannot do without; DRAM moves 8 % more than that,
 // and what is left is the latency of a row's loads (warps wait for them 8 cycles per instruction).  The
 // same rows each in a cluster's registers took 1463 us.  A block takes one row, or few: the rows without
 // weight then leave their room to others (persistent blocks: 797).
@@ -914,8 +914,9 @@ int stream_threads(int64_t V) {
 
 // The kernel by the vocabulary: lane groups with 8 logits a lane, then a warp with 16 (65,536 rows of 500
 // bf16: 83 us against 93 streamed), then streamed rows (of 1024: 88 against 179 with 32 a lane); rows of 128
-// KB and more that are too few to fill the GPU, in clusters (131,072 bf16 logits, 8 rows: 19 against 26 us;
-// at 19 rows, more than one wave of clusters, 26 against 25).
+// KB and more that are too few to fill the GPU, in clusters.  On the GPU, without the host's part, clusters
+// against streamed rows: 131,072 bf16 logits 8 rows 7.9 / 14.6 us, 16 rows 13.5 / 15.3, 32 rows 20.2 / 15.3; of 65,536
+// 6.6 / 9.4, 11.4 / 9.4, 16.0 / 9.9; 131,072 fp32 9.1 / 22.6, 15.7 / 23.5, 23.4 / 23.6.
 template <class T>
 cudaError_t token_rows(const TokenArgs& a, int& parts, cudaStream_t s) {
   if (a.V <= 32) return token_lanes<T, 4, 8>(a, parts, s);

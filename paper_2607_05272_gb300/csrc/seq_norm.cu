@@ -12,7 +12,10 @@
 // its output, in units of 8 columns per thread.
 // Measured on one GB300 (floors at 6783 GB/s), bf16 with p = 0.1: forward 16,384 x 4096 90 us (79), backward
 // 124 (99); rows that are off the 16-byte grid, 16,384 x 2047: 83 (40) and 117 (50), by instructions (74 per
-// element backward: partial units, sums in shared memory because columns move between threads).
+// element backward: partial units, sums in shared memory because columns move between threads).  fp32 16,384 x
+// 4096: 187 (158) and 214 (198).  Narrow rows leave lanes of their warp idle: 131,072 x 64 fp32 56 (20) and 70
+// (25); fp32 rows of more than 8192 columns hold more than their registers: 4096 x 16,384 210 (158) and 354 (198),
+// off the grid 4096 x 16,383 371 and 578.
 #include <algorithm>
 
 #include "kernels.h"

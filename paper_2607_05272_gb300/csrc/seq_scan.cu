@@ -17,7 +17,7 @@
 // s -> A s + B across its threads (and, where there are few columns and many steps, across a cluster of
 // blocks that share the steps), and applies the state that comes in to the same registers.
 // Measured on one GB300 (floors at 6783 GB/s): forward 2 x 65,536 steps x 1024 channels bf16 165 us (119);
-// backward 1024 x 512 x 64 fp32, time-major with episode ends, 142 (119) and 16 x 2048 x 2048 bf16 162 (119);
+// backward 1024 x 512 x 64 fp32, time-major with episode ends, 143 (119) and 16 x 2048 x 2048 bf16 163 (119);
 // one step of 256 x 2048 bf16 3.0 on the GPU, where the call's arguments take the host 10.5.
 #include <algorithm>
 #include <initializer_list>
@@ -979,8 +979,8 @@ constexpr int kFwdWarps = 8, kFwdPerSm = 2, kGradWarps = 4, kGradPerSm = 3;
 // (microseconds, measured over calls of 9 to 1770 MB: tiles of aligned tensors 3.4 to 5, of others 0.8 to
 // 1.3 with a quarter of the elements; wide tiles 2.4 forward and 3.5 backward, off alignment 3.2 to 5.4 and
 // 8.4 to 11, and up to a quarter more for a cluster's posts).  One long bf16 sequence of 18 channels, 17 x
-// 32,774 steps: clusters of 8 148 us, tiles 421; 115 x 6961 of 167 channels: tiles 306, clusters 436;
-// backward 16 x 2048 x 2048: clusters of 1, 2, 4, 8 201, 169, 167, 193.
+// 32,774 steps: clusters of 8 109 us, tiles 418; 115 x 6961 of 167 channels: tiles 308, clusters 439;
+// backward 16 x 2048 x 2048: clusters of 1, 2, 4, 8 199, 171, 167, 194.
 struct ScanPlan {
   bool columns, wide;
   int lcl, warps, cluster;
