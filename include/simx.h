@@ -575,8 +575,9 @@ typedef struct simx_seq {
  *   a_t = sigmoid(gate_t + bias_c),  h_t = a_t s_t + (1 - a_t) x_t,
  *   s_0 = h0 (NULL: zeros),  s_t = done_{t-1} ? 0 : h_{t-1},
  * as in compute_returns_gae, done_t != 0 ends the episode after step t (whatever h_t holds is then
- * dropped).  It is evaluated as s_t + (1 - a_t)(x_t - s_t), which keeps long memories exact; a state
- * that is not finite becomes NaN.  h_last [batch][channels] = the state that the next call continues from (h0 there):
+ * dropped).  It is evaluated as s_t + (1 - a_t)(x_t - s_t), which keeps long memories exact; a gate that
+ * forgets a state leaves the rounding of that difference behind, some 2^-23 of the larger of |s_t| and
+ * |x_t|.  A state that is not finite becomes NaN.  h_last [batch][channels] = the state that the next call continues from (h0 there):
  * done_{len-1} ? 0 : h_{len-1}, and h0 for len == 0; it is the unrounded state, and it may be h0's own
  * buffer.  Long sequences are shared by blocks that wait for each other's parts, about a second each at
  * most; past that the states (backward: the lambdas) that come from other blocks are NaN, and with them
