@@ -337,8 +337,9 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
       }
       tcx::fence_after();
       if (lane == 0) {
+        // In the last chunk too: its own o goes where that of the chunk before was.
+        if (!half) out_has_left();
         if (!half && n + 1 < chunks) {
-          out_has_left();
           copy(n + 1, 1, place(4));
           copy(n + 1, 2, place(5));
         }
@@ -363,7 +364,8 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
       __syncwarp();
     }
   };
-  // o of a chunk from shared memory, once it is there.
+  // o of a chunk from shared memory, once it is there.  It has left (multiply_state) before the products are done that
+  // put_out waits for, so that the next o may be written, and before another copy takes its place.
   auto out_whole = [&](int n) { return all.p[pass].o_tma && p1 - p0 - n * C >= C; };
   auto store_out = [&](int n) {
     bar_sync<NT + 32>(kOut);
