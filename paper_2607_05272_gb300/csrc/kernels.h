@@ -296,7 +296,6 @@ struct AttnPass {
   void* o;                   // of `dtype`, or fp32 where o_f32
   int64_t osb, ost, osh;
   int o_f32;
-  int exact;                 // a state that may be given out
   float inject, out_scale;
   const float* ld;
   const uint8_t* done;

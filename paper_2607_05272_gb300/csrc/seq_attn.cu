@@ -613,7 +613,6 @@ cudaError_t launch_attn(const simx_attention& a, void* ws, cudaStream_t s) {
   P.out_scale = a.scale;
   P.s_in = a.s0;
   P.s_out = a.s_last;
-  P.exact = 1;
   P.sx = a.dv;
   P.sy = 1;
   P.seg_state = static_cast<float*>(ws);
@@ -688,7 +687,6 @@ cudaError_t launch_attn_grad(const simx_attention& a, void* ws, cudaStream_t s) 
     }
   }
   V.s_out = a.ds0;
-  V.exact = 1;
   cudaError_t e;
   if ((e = run_passes(all, 3, shares_at(p, ws), s)) != cudaSuccess) return e;
   if (group == 1) return cudaSuccess;

@@ -3,11 +3,12 @@
 // Chunks of 128 steps of one head, with the state S in registers; four products a chunk on tcgen05.mma with
 // FP32 accumulators in tensor memory:
 //   scores = a b^T,  far = a S,  o = (scores * link) c + reach far,  S' = keep S + (b * link to the end)^T c.
-// The inputs are operands as they are.  What is computed (links times scores, states, weighted b) has more digits
-// than bf16 and is an operand in parts, x = x1 + x2 (+ x3), each part the next digits that bf16 holds: two parts
-// where a result is rounded to bf16 anyway (2^-16 of each term), three in passes whose state may be asked for in
-// fp32 (all of fp32's digits), so that o is the same whether it is or not.  fp32 inputs would take six products of parts for each: they go to the FP32 units
-// (seq_attn.cu).
+// The inputs are operands as they are.  What is computed has more digits than bf16 and is an operand in parts, x =
+// x1 + x2 (+ x3), each part the next digits that bf16 holds: three (all of fp32's digits) for weighted b, which is added to
+// the state, in every pass; two for links times scores and for the state in `far`, whose products go to a result that is
+// rounded to bf16 anyway (2^-16 of each term; a third part of either would take columns of tensor memory that dimensions
+// of 64 do not have and shared memory that dimensions of 128 do not have).  fp32 inputs would take six products of parts
+// for each: they go to the FP32 units (seq_attn.cu).
 //
 // Operands lie in shared memory step by step, in columns of 64 elements (32 where D is 32) whose 16-byte units
 // are permuted within each 8 steps (the 128-byte and 64-byte swizzle): the same bytes are an operand along the
@@ -291,7 +292,6 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
                (int)(h / (k == 0 ? A.adiv : k == 1 ? A.bdiv : A.cdiv)) * A.head_step[k], (int)b * A.batch_step[k], &full[k]);
   };
   auto out_has_left = [&]() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); };
-  auto exact = [&]() { return KEEP || all.p[pass].exact; };  // whether the state is in three parts
   // Products of parts go from the smallest to the largest: sums in tensor memory are cut off, by 2^-23 of what they
   // have come to.  First those with a, of chunk n at operands at_a, at_b; the next chunk's a is copied to at_next.
   auto multiply_a = [&](int n) {
@@ -352,7 +352,6 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
         uint32_t acc = half;
 #pragma unroll
         for (int p = 2; p >= 0; --p) {
-          if (p == 2 && !exact()) continue;
 #pragma unroll
           for (int k = 0; k < C / 2; k += 16) {
             tcx::mma_bf16(tm + S::kFar, bt_desc[p] + (step_at(k) >> 4), ct_desc + (step_at(k) >> 4), id, acc);
@@ -742,8 +741,7 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = nan();  // its c is zeros
           *reinterpret_cast<uint4*>(p) = take8(v);
-          if (exact()) store_parts<2>(v, q, S::kTile);
-          else store_parts<1>(v, q, S::kTile);
+          store_parts<2>(v, q, S::kTile);
         }
       }
       tcx::fence_async_smem();

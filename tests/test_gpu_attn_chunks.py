@@ -69,3 +69,33 @@ def test_rows_leave_whole_while_memory_is_busy(simx, B, T, H, D):
             _call_grad(simx, q, k, v, go, ld, ws=wb, g=g)
             assert all(torch.equal(a, b) for a, b in zip((o, last, *g), ref))
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("D", [24, 64, 128])
+def test_states_of_a_gradient_keep_their_digits(simx, D):
+    """grad_q where what the steps add to the state cancels: steps 40, 140 and 200 leave some 2^-18 of what each
+    added.  Tolerance, of the sum of absolute terms: a power of the decay is off by 2^-22, twice; products and sums in
+    fp32 by 2^-24, four of them; three parts added up by 2^-23 each, cut off: (4 + 2 + 3) 2^-23 < 2^-19.  On the result
+    itself 2^-16 for the state as an operand and 2^-8 for its rounding to bf16."""
+    B, T, H = 4, 300, 8
+    r = np.random.default_rng(D)
+    ld = -np.exp(r.uniform(np.log(1e-3), np.log(2e-2), H)).astype(np.float32)
+    lam = np.exp(ld.astype(np.float64))[None, :, None]
+    bf = lambda x: torch.from_numpy(x).bfloat16()  # noqa: E731
+    v, k = torch.zeros(B, T, H, D), torch.zeros(B, T, H, D)
+    k[:, [40, 140, 200]] = bf(r.standard_normal((B, 1, H, D))).float()
+    v[:, 40] = bf(r.standard_normal((B, H, D))).float()
+    left, at = v[:, 40].double().numpy(), 40
+    for t in (140, 200):
+        left, at = left * lam ** (t - at), t
+        v[:, t] = bf(-left).float()
+        left = left + v[:, t].double().numpy()
+    go = torch.zeros(B, T, H, D)
+    rows = np.arange(256, T)
+    go[:, rows, :, rows % D] = 1.0
+    q, k, v, go = (x.cuda().bfloat16() for x in (torch.zeros(B, T, H, D), k, v, go))
+    g = _call_grad(simx, q, k, v, go, torch.from_numpy(ld).cuda(), scale=1.0)
+    ref = attn.decay_attention_grad(_f64(q), _f64(k), _f64(v), _f64(go), ld.astype(np.float64), 1.0)
+    got, want, size = _f64(g[0]), ref["grad_q"], ref["grad_q_size"]
+    assert (np.abs(want).sum() < 2.0 ** -15 * size.sum()) and want[:, rows].any()
+    assert (np.abs(got - want) <= 2.0 ** -19 * size + (2.0 ** -8 + 2.0 ** -16) * np.abs(want)).all()
