@@ -4,9 +4,9 @@
 // FP32 accumulators in tensor memory:
 //   scores = a b^T,  far = a S,  o = (scores * link) c + reach far,  S' = keep S + (b * link to the end)^T c.
 // The inputs are operands as they are.  What is computed has more digits than bf16 and is an operand in parts, x =
-// x1 + x2 (+ x3), each part the next digits that bf16 holds: three (all of fp32's digits) for weighted b, which is added to
+// x1 + x2 (+ x3), each part what is left so far, rounded to bf16: three (all of fp32's digits) for weighted b, which is added to
 // the state, in every pass; two for links times scores and for the state in `far`, whose products go to a result that is
-// rounded to bf16 anyway (2^-16 of each term; a third part of either would take columns of tensor memory that dimensions
+// rounded to bf16 anyway (2^-17 of each term; a third part of either would take columns of tensor memory that dimensions
 // of 64 do not have and shared memory that dimensions of 128 do not have).  fp32 inputs would take six products of parts
 // for each: they go to the FP32 units (seq_attn.cu).
 //
@@ -52,13 +52,11 @@ __device__ __forceinline__ float high(uint32_t u) { return __uint_as_float(u & 0
 
 __device__ __forceinline__ void unpair(Pair v, float& x, float& y) { x = halves(v).x, y = halves(v).y; }
 
-// The upper eight digits of (x, y) as a part, and what is left of them: a mask costs less than a rounding to
-// bf16, and the last part (pack2) is rounded.
+// (x, y) rounded to bf16 as a part, and what is left of them.
 __device__ __forceinline__ uint32_t take(float& x, float& y) {
-  uint32_t u;
-  asm("prmt.b32 %0, %1, %2, 0x7632;" : "=r"(u) : "r"(__float_as_uint(x)), "r"(__float_as_uint(y)));
+  const uint32_t u = pack2(x, y);
   Pair r;
-  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(x, y)), "l"(pair(__uint_as_float(__float_as_uint(x) & 0xffff0000u), __uint_as_float(__float_as_uint(y) & 0xffff0000u))));
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(x, y)), "l"(pair(low(u), high(u))));
   unpair(r, x, y);
   return u;
 }

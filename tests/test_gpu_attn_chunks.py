@@ -99,3 +99,25 @@ def test_states_of_a_gradient_keep_their_digits(simx, D):
     got, want, size = _f64(g[0]), ref["grad_q"], ref["grad_q_size"]
     assert (np.abs(want).sum() < 2.0 ** -15 * size.sum()) and want[:, rows].any()
     assert (np.abs(got - want) <= 2.0 ** -19 * size + (2.0 ** -8 + 2.0 ** -16) * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_a_state_as_an_operand(simx, D):
+    """q S where rows of the state cancel.  Both parts are rounded: the first leaves at most 2^-8 of a power of two
+    below the number, the second half a step of that, 2^-17; sums add 2^-23 each, cut off, eight of them at most; past the
+    first chunk the state was multiplied by a power of the decay, 2^-22; another one and the rounding to bf16 are 2^-20 and
+    2^-8 of the result itself."""
+    B, T, H = 2, 200, 4
+    r = np.random.default_rng(D + 1)
+    s0 = r.standard_normal((B, H, D, D)).astype(np.float32)
+    s0[:, :, 1::2] = s0[:, :, ::2] * (1 + 2.0 ** -12 * r.standard_normal((B, H, D // 2, D))).astype(np.float32)
+    ld = np.float32([-1e-3, -1e-4, 0.0, -3e-3])
+    q = np.zeros((B, T, H, D), np.float32)
+    x = 2 * (np.arange(T) % (D // 2))
+    q[:, np.arange(T), :, x], q[:, np.arange(T), :, x + 1] = 1.0, -1.0
+    q = torch.from_numpy(q).cuda().bfloat16()
+    zero = torch.zeros_like(q)
+    o, last = _call(simx, q, zero, zero, torch.from_numpy(ld).cuda(), s0=torch.from_numpy(s0).cuda(), scale=1.0)
+    ref = attn.decay_attention(_f64(q), _f64(zero), _f64(zero), ld.astype(np.float64), 1.0, s0.astype(np.float64))
+    err = (2.0 ** -17 + 8 * 2.0 ** -23 + 2.0 ** -22) * ref["o_size"] + (2.0 ** -8 + 2.0 ** -20) * np.abs(ref["o"])
+    assert (np.abs(_f64(o) - ref["o"]) <= err).all()
