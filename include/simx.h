@@ -681,14 +681,16 @@ typedef struct simx_heads {
  * What no link reaches counts for nothing, whatever it holds: later steps, other episodes, the state
  * before an end.  Where a step counts whose key or value is not finite, the result is not finite either.
  * Finite inputs give finite results where states and products of a key and a value stay below 2^123.
- * s0, done and s_last may be NULL.  An empty problem (batch or heads 0) touches nothing.
+ * s0, done and s_last may be NULL.  o lies apart from q, k and v, and s_last from s0 unless it is s0.  An empty
+ * problem (batch or heads 0) touches nothing.
  *
  * simx_decay_attention_grad: given grad_o (the gradient of o) and ds_last (of s_last; NULL: zeros),
  *   R_t = scale q_t^T grad_o_t + (done_t ? 0 : t + 1 < len ? lambda R_{t+1} : ds_last),
  *   grad_q_t = scale S_t grad_o_t,  grad_k_t = R_t v_t,  grad_v_t = k_t R_t,
  *   ds0 = lambda R_0 (ds_last for len == 0),
  * grad_k and grad_v summed over the heads that share them, in the heads' order, and rounded once.  The
- * decays are given, not learned.  ds_last and ds0 may be NULL and lie apart.
+ * decays are given, not learned.  ds_last and ds0 may be NULL.  No output lies in place of an input: the
+ * gradients lie apart from q, k, v, grad_o and one another, ds0 from s0 and ds_last.
  */
 typedef struct simx_attention {
   int64_t batch, len, heads, kv_heads, dk, dv;

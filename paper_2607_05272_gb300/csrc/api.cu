@@ -1201,6 +1201,56 @@ static simx_status check_heads(const simx_attention* a, const simx_heads& q, int
   return SIMX_OK;
 }
 
+// A tensor of an attention with its sizes.
+struct HeadsOf {
+  const simx_heads* t;
+  int64_t heads, dim;
+  const char* name;
+  bool output;
+};
+
+// Whether off = sum of i stride over the axes + d, with -below <= i <= above for each axis and -lo <= d <= hi.
+struct Gap {
+  int64_t stride, below, above;
+};
+static bool steps_to(int64_t off, const Gap* axis, int n, int64_t lo, int64_t hi) {
+  if (n == 0) return -lo <= off && off <= hi;
+  const int64_t i = off / axis->stride;
+  for (int64_t j = i - 1; j <= i + 1; ++j)
+    if (-axis->below <= j && j <= axis->above && steps_to(off - j * axis->stride, axis + 1, n - 1, lo, hi)) return true;
+  return false;
+}
+
+// Whether two tensors share an element, as far as that is found at once: where they start at the same address or step by
+// the same strides (parts of one packed buffer do, and lie apart).
+static bool share_elements(const simx_attention& a, const HeadsOf& x, const HeadsOf& y) {
+  if (x.t->p == y.t->p) return true;
+  if (x.t->sb != y.t->sb || x.t->st != y.t->st || x.t->sh != y.t->sh) return false;
+  const int64_t bytes = (int64_t)(reinterpret_cast<uintptr_t>(y.t->p) - reinterpret_cast<uintptr_t>(x.t->p)), es = elem_bytes(a.dtype);
+  Gap axis[3];
+  int n = 0;
+  for (const Gap& g : {Gap{x.t->sb, a.batch - 1, a.batch - 1}, Gap{x.t->st, a.len - 1, a.len - 1}, Gap{x.t->sh, y.heads - 1, x.heads - 1}})
+    if (g.stride > 0) axis[n++] = g;
+  std::sort(axis, axis + n, [](const Gap& p, const Gap& q) { return p.stride > q.stride; });
+  return steps_to(bytes / es, axis, n, y.dim - 1, x.dim - 1);
+}
+
+static bool ranges_meet(const void* p, const void* q, double bytes) {
+  const uintptr_t u = reinterpret_cast<uintptr_t>(p), v = reinterpret_cast<uintptr_t>(q);
+  return p && q && (double)(u > v ? u - v : v - u) < bytes;
+}
+
+static double state_bytes(const simx_attention& a) { return 4.0 * (double)a.batch * (double)a.heads * (double)a.dk * (double)a.dv; }
+
+// Whether no output shares elements with another tensor.
+static simx_status check_apart(const simx_attention& a, const HeadsOf* all, int n) {
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j)
+      if (all[i].output && i != j && (!all[j].output || j < i) && share_elements(a, all[i], all[j]))
+        return fail(SIMX_EINVAL, "%s overlaps %s", all[i].name, all[j].name);
+  return SIMX_OK;
+}
+
 static simx_status check_attention(const simx_attention* a) {
   if (!a) return fail(SIMX_EINVAL, "attention arguments are NULL");
   if (!elem_bytes(a->dtype)) return fail(SIMX_EINVAL, "dtype %d", a->dtype);
@@ -1247,11 +1297,13 @@ simx_status simx_decay_attention(const simx_attention* a, void* d_workspace, siz
   if (v != SIMX_OK) return v;
   if (a->batch == 0 || a->heads == 0) return SIMX_OK;
   if (a->len > 0) {
-    if ((v = check_heads(a, a->q, a->heads, a->dk, "q", false)) != SIMX_OK) return v;
-    if ((v = check_heads(a, a->k, a->kv_heads, a->dk, "k", false)) != SIMX_OK) return v;
-    if ((v = check_heads(a, a->v, a->kv_heads, a->dv, "v", false)) != SIMX_OK) return v;
-    if ((v = check_heads(a, a->o, a->heads, a->dv, "o", true)) != SIMX_OK) return v;
+    const HeadsOf all[] = {{&a->q, a->heads, a->dk, "q", false}, {&a->k, a->kv_heads, a->dk, "k", false}, {&a->v, a->kv_heads, a->dv, "v", false},
+                           {&a->o, a->heads, a->dv, "o", true}};
+    for (const HeadsOf& t : all)
+      if ((v = check_heads(a, *t.t, t.heads, t.dim, t.name, t.output)) != SIMX_OK) return v;
+    if ((v = check_apart(*a, all, 4)) != SIMX_OK) return v;
   }
+  if (a->s_last != a->s0 && ranges_meet(a->s_last, a->s0, state_bytes(*a))) return fail(SIMX_EINVAL, "s_last overlaps s0");
   v = check_workspace(d_workspace, workspace_bytes, attn_workspace_bytes(a->batch, a->len, a->heads, a->kv_heads, a->dk, a->dv));
   if (v != SIMX_OK) return v;
   cudaError_t e = launch_attn(*a, d_workspace, (cudaStream_t)stream);
@@ -1264,14 +1316,16 @@ simx_status simx_decay_attention_grad(const simx_attention* a, void* d_workspace
   if (v != SIMX_OK) return v;
   if (a->batch == 0 || a->heads == 0) return SIMX_OK;
   if (a->len > 0) {
-    const struct { const simx_heads* q; int64_t heads, dim; const char* name; bool output; } all[] = {
+    const HeadsOf all[] = {
         {&a->q, a->heads, a->dk, "q", false}, {&a->k, a->kv_heads, a->dk, "k", false}, {&a->v, a->kv_heads, a->dv, "v", false},
         {&a->grad_o, a->heads, a->dv, "grad_o", false}, {&a->grad_q, a->heads, a->dk, "grad_q", true},
         {&a->grad_k, a->kv_heads, a->dk, "grad_k", true}, {&a->grad_v, a->kv_heads, a->dv, "grad_v", true}};
-    for (const auto& t : all)
-      if ((v = check_heads(a, *t.q, t.heads, t.dim, t.name, t.output)) != SIMX_OK) return v;
+    for (const HeadsOf& t : all)
+      if ((v = check_heads(a, *t.t, t.heads, t.dim, t.name, t.output)) != SIMX_OK) return v;
+    if ((v = check_apart(*a, all, 7)) != SIMX_OK) return v;
   }
-  if (a->ds0 && a->ds0 == a->ds_last) return fail(SIMX_EINVAL, "ds0 is ds_last's own buffer");
+  for (const float* s : {a->ds_last, a->s0})
+    if (ranges_meet(a->ds0, s, state_bytes(*a))) return fail(SIMX_EINVAL, "ds0 overlaps %s", s == a->s0 ? "s0" : "ds_last");
   v = check_workspace(d_workspace, workspace_bytes, attn_grad_workspace_bytes(a->batch, a->len, a->heads, a->kv_heads, a->dk, a->dv));
   if (v != SIMX_OK) return v;
   cudaError_t e = launch_attn_grad(*a, d_workspace, (cudaStream_t)stream);
