@@ -676,10 +676,12 @@ typedef struct simx_heads {
  * `done` ends episodes as in simx_gated_scan; sequences packed into one row are episodes too.  s_last
  * [batch][heads][dk][dv] = the state that the next call continues from (s0 there): done_{len-1} ? 0 :
  * S_{len-1}, and s0 for len == 0; it may be s0's own buffer.  len == 1 is the single-token step of serving.
- * States are fp32.  log_decay [heads] is at most 0 (-inf: no memory); another value gives NaN in all
- * that its head puts out.  1 <= dk, dv <= 128; kv_heads divides heads.  q, k and v may have strides of zero.
+ * States are fp32.  log_decay [heads] is at most 0 (-inf and all below -104, where lambda is 0 in fp32: no
+ * memory); another value gives NaN in all that its head puts out.  1 <= dk, dv <= 128; kv_heads divides
+ * heads.  q, k and v may have strides of zero.
  * What no link reaches counts for nothing, whatever it holds: later steps, other episodes, the state
- * before an end.  Where a step counts whose key or value is not finite, the result is not finite either.
+ * before an end, without a memory all other steps.  Where a step counts whose key or value is not finite, the
+ * result is not finite either, at distances whose power of lambda is above 0 in fp32 at least.
  * Finite inputs give finite results where states and products of a key and a value stay below 2^123.
  * s0, done and s_last may be NULL.  o lies apart from q, k and v, and s_last from s0 unless it is s0.  An empty
  * problem (batch or heads 0) touches nothing.

@@ -751,8 +751,9 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
         gather(n + 1, 2, place(5));
       }
       if (!KEEP) {
-        // (3) links times scores, over the scores
-        const int least = -(int)__reduce_max_sync(0xffffffffu, -max(first, 0)), most = (int)__reduce_max_sync(0xffffffffu, max(first, 0));
+        // (3) links times scores, over the scores.  Without a memory a step is linked to itself alone.
+        const int since = pw[1] == 0.0f ? i : max(first, 0);
+        const int least = -(int)__reduce_max_sync(0xffffffffu, -since), most = (int)__reduce_max_sync(0xffffffffu, since);
 #pragma unroll 1
         for (int j0 = 16 * side; j0 < C; j0 += 16 * S::kSides) {
           uint32_t u[16];
@@ -784,7 +785,7 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
                 const int j = flip ? lo + 15 - e : lo + e;
-                w[e] = j < first ? 0.0f : check && j <= i && bad[n & 1][j0 + e] ? nan() : w[e];
+                w[e] = j < since ? 0.0f : check && j <= i && bad[n & 1][j0 + e] ? nan() : w[e];
               }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {

@@ -121,3 +121,29 @@ def test_a_state_as_an_operand(simx, D):
     ref = attn.decay_attention(_f64(q), _f64(zero), _f64(zero), ld.astype(np.float64), 1.0, s0.astype(np.float64))
     err = (2.0 ** -17 + 8 * 2.0 ** -23 + 2.0 ** -22) * ref["o_size"] + (2.0 ** -8 + 2.0 ** -20) * np.abs(ref["o"])
     assert (np.abs(_f64(o) - ref["o"]) <= err).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,at", [(5, 2), (9, 3), (150, 60), (300, 127), (300, 128), (300, 250)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_no_memory_links_no_step(simx, T, at, bad, dtype):
+    """Decays that are 0 in fp32: a step that is not finite reaches itself alone, forward and backward, whatever its
+    place in a chunk; neither do s0 and other steps."""
+    B, H, D = 2, 5, 24
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    clean = [torch.randn((B, T, H, D), generator=gen, device="cuda").to(dtype) for _ in range(4)]
+    ld = torch.tensor([-float("inf"), -200.0, -110.0, -1e30, -0.1], device="cuda")
+    s0 = torch.randn((B, H, D, D), generator=gen, device="cuda")
+    ref = [*_call(simx, *clean[:3], ld, s0=s0), *_call_grad(simx, *clean, ld, s0=s0)]
+    assert all(torch.isfinite(x).all() for x in ref)
+    for i in range(4):
+        t = [x.clone() for x in clean]
+        t[i][0, at, :4, 3] = bad
+        got = [*_call(simx, *t[:3], ld, s0=s0), *_call_grad(simx, *t, ld, s0=s0)]
+        hit = torch.zeros((B, T, H), dtype=torch.bool, device="cuda")
+        hit[0, at, :4] = True
+        for n, (x, y) in enumerate(zip(got, ref)):
+            assert torch.equal(x, y) if n in (1, 5) else torch.equal(x[~hit], y[~hit])  # the states, all of them
+        o, gq, gk, gv = got[0][hit], *(x[hit] for x in got[2:5])
+        assert not torch.isfinite(o).all() or i == 3
+        assert not (torch.isfinite(gq).all() and torch.isfinite(gk).all() and torch.isfinite(gv).all())
