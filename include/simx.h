@@ -682,7 +682,10 @@ typedef struct simx_heads {
  * What no link reaches counts for nothing, whatever it holds: later steps, other episodes, the state
  * before an end, without a memory all other steps.  Where a step counts whose key or value is not finite, the
  * result is not finite either, at distances whose power of lambda is above 0 in fp32 at least.
- * Finite inputs give finite results where states and products of a key and a value stay below 2^123.
+ * Finite inputs give finite results where states and products of a key and a value stay below 2^123.  In
+ * bf16, sequences of more than 8 steps go by chunks that form products of queries and keys before those with
+ * values: there the sum of |q k| over a head's elements stays below 2^123 too, in a gradient of any length that and
+ * the sum of |v grad_o|, and what falls below fp32's range in these products is lost.
  * s0, done and s_last may be NULL.  o lies apart from q, k and v, and s_last from s0 unless it is s0.  An empty
  * problem (batch or heads 0) touches nothing.
  *

@@ -9,6 +9,7 @@
 // rounded to bf16 anyway (2^-17 of each term; a third part of either would take columns of tensor memory that dimensions
 // of 64 do not have and shared memory that dimensions of 128 do not have).  fp32 inputs would take six products of parts
 // for each: they go to the FP32 units (seq_attn.cu).
+// Scores are sums in fp32 before they meet c: the sizes of a and b are bounded together, unlike step by step.
 //
 // Operands lie in shared memory step by step, in columns of 64 elements (32 where D is 32) whose 16-byte units
 // are permuted within each 8 steps (the 128-byte and 64-byte swizzle): the same bytes are an operand along the

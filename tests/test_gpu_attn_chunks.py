@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 from oracle import attn
+from tests.test_gpu_attn import _close, _state
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -147,3 +148,31 @@ def test_no_memory_links_no_step(simx, T, at, bad, dtype):
         o, gq, gk, gv = got[0][hit], *(x[hit] for x in got[2:5])
         assert not torch.isfinite(o).all() or i == 3
         assert not (torch.isfinite(gq).all() and torch.isfinite(gk).all() and torch.isfinite(gv).all())
+
+
+@pytest.mark.parametrize("D", [32, 128])
+@pytest.mark.parametrize("small", ["v", "go"])
+def test_large_scores(simx, D, small):
+    """Queries and keys whose products come near to the largest that the chunks take (|v grad_o| in the same way), with
+    values as small: test_gpu_attn's bounds."""
+    B, T, H = 2, 300, 2
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    q, k, v, go = (torch.randn((B, T, H, D), generator=gen, device="cuda") for _ in range(4))
+    # the sum over a head's elements: below 128 * 5 * 5 * 2^110 < 2^123
+    if small == "v":
+        q, k, v, go = q * 2.0 ** 55, k * 2.0 ** 55, v * 2.0 ** -80, go * 2.0 ** -30
+    else:
+        q, k, v, go = q * 2.0 ** -70, k * 2.0 ** -40, v * 2.0 ** 50, go * 2.0 ** 60
+    q, k, v, go = (x.bfloat16() for x in (q, k, v, go))
+    ld = torch.tensor([-0.01, -0.3], device="cuda")
+    done = (torch.rand((B, T), generator=gen, device="cuda") < 0.01).to(torch.uint8)
+    o, last = _call(simx, q, k, v, ld, done=done)
+    g = _call_grad(simx, q, k, v, go, ld, done=done)
+    sc, d = np.float64(np.float32(D ** -0.5)), done.cpu().numpy()
+    ref = attn.decay_attention(_f64(q), _f64(k), _f64(v), _f64(ld), sc, None, d)
+    _close(_f64(o), ref["o"], ref["o_size"], "bf16", T, "o")
+    _state(_f64(last), ref["s_last"], ref["s_last_size"], T, "s_last")
+    ref = attn.decay_attention_grad(_f64(q), _f64(k), _f64(v), _f64(go), _f64(ld), sc, None, d)
+    for n, x in zip(("grad_q", "grad_k", "grad_v"), g):
+        _close(_f64(x), ref[n], ref[n + "_size"], "bf16", T, n)
+    _state(_f64(g[3]), ref["ds0"], ref["ds0_size"], T, "ds0")
