@@ -3,9 +3,11 @@
 // Per row of logits x, with a reference m near its maximum and the temperature T:
 //   s = sum e^((x - m) / T), t = sum e^((x - m) / T) (x - m),
 //   log pi(a) = (x_a - m) / T - log s, H = log s - t / (s T).
-// Each thread keeps a reference of its own, moved when a term would pass 2^60, and its sums are moved to the
-// row's once.  Terms are added eight at a time from zero, and these to a sum that keeps its rounding errors: one
-// running sum lost the many small terms beside a large one (4e-6 of the entropy; now 5e-7).
+// Each thread keeps a reference of its own, moved when a term would pass 2^8, and its sums are moved to the row's
+// maximum once, so that neither difference above loses digits: with references as far as 2^60 below the maximum, log pi
+// of a peak was off by 4e-6 where it is near 0.  Terms are added eight at a time from zero, and these to a sum that keeps
+// its rounding errors: one running sum lost the many small terms beside a large one.  Entropies are off by 9e-7 at most
+// with references within 2^8, by 3.5e-6 within 2^16; moving them that often costs 1 % of the time.
 //
 // The largest logits take no work in that pass but each thread's largest.  If t threads of each of w warps hold
 // logits at or above a bound, and t w >= top, every logit sought is at or above it, and so is among the logits of the
@@ -13,7 +15,7 @@
 // logit in order-preserving bits above the complement of its index, so that equal logits rank by index and no two
 // keys are equal; each warp keeps its largest in a list, a key to a lane, and one warp merges the lists.
 //
-// Bound by instructions: 8192 rows of 50001 bf16 in 208 us, 59 % of the copy rate, with 21,800 warp instructions to a row
+// Bound by instructions: 8192 rows of 50001 bf16 in 211 us, 58 % of the copy rate, with 21,800 warp instructions to a row
 // (issue 68 % of the time), of which joins, candidates and their ranking are a third; of 131072 in 426 us, 75 %.
 // Logits go in pairs, each with one exponential.  40 registers instead of 48, for more warps, spill: 223 us.
 #include <algorithm>
@@ -30,6 +32,7 @@ namespace {
 constexpr int kRows = 8;       // of a block, with a warp for each
 constexpr int kWarps = 8;      // of a row that a block has
 constexpr int kMostRanks = 8;  // blocks of a cluster
+constexpr float kLag = 8.0f;   // octaves by which a thread's largest term may pass its reference
 
 typedef unsigned long long Key;
 
@@ -56,13 +59,15 @@ __device__ __forceinline__ void move_to(Sums& a, float m, float k) {
   }
   a.m = m;
 }
-__device__ __forceinline__ Sums join_lanes(Sums a, float k) {
-  move_to(a, max_lanes(a.m), k);
+// `most`: the largest that a lane has seen.
+__device__ __forceinline__ Sums join_lanes(Sums a, float most, float k) {
+  move_to(a, max_lanes(most), k);
   return {a.m, sum_lanes(a.s), sum_lanes(a.t)};
 }
 // Of n parts, a lane each.
 __device__ __forceinline__ Sums join_parts(const Sums* part, int n, int lane, float k) {
-  return join_lanes(lane < n ? part[lane] : Sums{-inf(), 0.0f, 0.0f}, k);
+  const Sums a = lane < n ? part[lane] : Sums{-inf(), 0.0f, 0.0f};
+  return join_lanes(a, a.m, k);
 }
 
 // Puts a key into the list of a warp, in descending order over its lanes; the last one falls out.
@@ -194,7 +199,7 @@ __global__ void __launch_bounds__(NW == 1 ? 32 * kRows : 32 * NW) k_logprobs(con
 #pragma unroll
     for (int u = 1; u < U; ++u) m = fmaxf(m, e[u].most());
     best = fmaxf(best, m);
-    if (m > ref && !(__fmul_rn(__fsub_rn(m, ref), A.k) <= 60.0f)) {
+    if (m > ref && !(__fmul_rn(__fsub_rn(m, ref), A.k) <= kLag)) {
       Sums a = {ref, s.value(), t.value()};
       move_to(a, m, A.k);
       s = {a.s, 0.0f};
@@ -231,7 +236,7 @@ __global__ void __launch_bounds__(NW == 1 ? 32 * kRows : 32 * NW) k_logprobs(con
       t.add(__fadd_rn(pt[0], pt[1]), 0.0f);
     }
   }
-  Sums sum = join_lanes({ref, s.value(), t.value()}, A.k);
+  Sums sum = join_lanes({ref, s.value(), t.value()}, best, A.k);
   Key mine = 0;
   if (top) {
     // the bound: the each-th largest of every warp's threads, the least of them
@@ -347,12 +352,12 @@ __global__ void __launch_bounds__(NW == 1 ? 32 * kRows : 32 * NW) k_logprobs(con
   if (lane == 0) {
     if (A.logp) {
       const bool known = !broken && tok >= 0 && tok < V;
-      A.logp[row] = known ? __fsub_rn(__fmul_rn(__fsub_rn(taken, sum.m), A.inv_t), logs) : nan();
+      A.logp[row] = known ? fminf(0.0f, __fsub_rn(__fmul_rn(__fsub_rn(taken, sum.m), A.inv_t), logs)) : nan();
     }
     if (A.entropy) A.entropy[row] = broken ? nan() : fmaxf(0.0f, __fsub_rn(logs, __fmul_rn(__fdiv_rn(sum.t, sum.s), A.inv_t)));
   }
   if (lane < top) {
-    if (A.top_logp) A.top_logp[row * top + lane] = broken ? nan() : __fsub_rn(__fmul_rn(__fsub_rn(key_value(mine), sum.m), A.inv_t), logs);
+    if (A.top_logp) A.top_logp[row * top + lane] = broken ? nan() : fminf(0.0f, __fsub_rn(__fmul_rn(__fsub_rn(key_value(mine), sum.m), A.inv_t), logs));
     if (A.top_index) A.top_index[row * top + lane] = broken ? -1 : (int64_t)(0xffffffffu - (uint32_t)mine);
   }
 }
