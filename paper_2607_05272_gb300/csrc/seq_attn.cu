@@ -59,10 +59,10 @@ __device__ __forceinline__ void store_row(float* p, const float (&v)[N]) {
 }
 
 // The state that a segment starts with, N elements of it: what the segments before it added, each times what the
-// ones between kept of it.  place(i, x, y): element i's row and column, false where there is none.  A segment's
+// ones between keep of it.  place(i, x, y): element i's row and column, false where there is none.  A segment's
 // elements are loaded together.
 template <int N, class Place>
-__device__ __forceinline__ void first_state(const AttnPass& A, int64_t bh, int seg, float (&s)[N], Place place) {
+__device__ __forceinline__ void first_state(const AttnPass& A, float ld, int64_t bh, int seg, float (&s)[N], Place place) {
 #pragma unroll
   for (int i = 0; i < N; ++i) s[i] = 0.0f;
   float w = 1.0f;
@@ -74,7 +74,7 @@ __device__ __forceinline__ void first_state(const AttnPass& A, int64_t bh, int s
       int x, y;
       if (place(i, x, y)) s[i] = __fmaf_rn(w, p[x * A.dc + y], s[i]);
     }
-    w = __fmul_rn(w, A.seg_keep[at_q]);
+    w = A.seg_keep[at_q] != 0.0f ? segments_keep(A, ld, q, seg) : 0.0f;
   }
   if (w == 0.0f || !A.s_in) return;
   const float* p = A.s_in + bh * A.da * A.dc;
@@ -128,7 +128,8 @@ __global__ void __launch_bounds__(32, Flat<X>::kBlocks) k_attn(const Passes all)
   // beside an end of an episode, steps go by themselves.
   const bool scaled = lam >= 0.5f;
   // The state then takes lambda^4 rounded to fp32, or the value beside it, whichever keeps the product of all so far
-  // nearest to the power: over a memory of 4096 steps roundings of the same sign would show.
+  // nearest to the power: over a memory of 4096 steps roundings of the same sign would show.  (The state's own roundings,
+  // 2^-24 every four steps, have one sign where lambda^4 is within some 2^-20 of 1 and little is added.)
   const float lam4 = power(ld, 4), rest = scaled ? __fmul_rn(4.0f, decay_rest(ld, lam, lam4)) : 0.0f;
   const float beside = __uint_as_float(__float_as_uint(lam4) + (rest > 0.0f ? 1 : -1));
   const float gap = rest != 0.0f ? fabsf(__fdiv_rn(__fsub_rn(beside, lam4), lam4)) : 1.0f;
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(32, Flat<X>::kBlocks) k_attn(const Passes all)
   Pair s[F::kPairs][CN];
   {
     float first[2 * F::kPairs * CN];
-    first_state(A, bh, KEEP ? 0 : seg, first, [&](int i, int& x, int& y) {
+    first_state(A, ld, bh, KEEP ? 0 : seg, first, [&](int i, int& x, int& y) {
       x = x0 + i / (2 * CN) * 2 + i % 2;
       y = y0 + i / 2 % CN;
       return !KEEP && x < A.da && y < A.dc;

@@ -19,9 +19,18 @@ __device__ __forceinline__ float power(float ld, int n) {
   return __fmaf_rn(e, __fmaf_rn(ld, (float)n, -p), e);
 }
 
-// What rounding took off lambda^n, given lambda and lambda^n in fp32: relative to it, a step.  A long memory would show it.
-// With u = 1 - lambda, exact from 1 / 2 on, log lambda + u + u^2 / 2 + ... is what the rounding of lambda took; below
-// 15 / 16 no memory is long.  n: 1 or 4.
+// What rounding took off e^l = v, relative to it; 0 below v = 3 / 4, where no memory is long.  With u = 1 - v, exact,
+// l - log v = l + u + u^2 / 2 + ..., whose first two terms cancel.
+__device__ __forceinline__ float power_rest(float l, float v) {
+  if (!(v >= 0.75f)) return 0.0f;
+  const float u = __fsub_rn(1.0f, v);
+  float f = 1.0f / 12.0f;
+#pragma unroll
+  for (int k = 11; k >= 2; --k) f = __fmaf_rn(u, f, 1.0f / (float)k);
+  return __fmaf_rn(__fmul_rn(u, u), f, __fadd_rn(l, u));
+}
+
+// The same of lambda^n given lambda and lambda^n in fp32, a step; below lambda = 15 / 16 nothing.  n: 1 or 4.
 __device__ __forceinline__ float decay_rest(float ld, float lam, float lam_n) {
   if (!(lam >= 0.9375f)) return 0.0f;
   if (lam_n == lam) {
@@ -32,11 +41,13 @@ __device__ __forceinline__ float decay_rest(float ld, float lam, float lam_n) {
     f = __fmaf_rn(u, f, 0.5f);
     return __fmaf_rn(__fmul_rn(u, u), f, __fadd_rn(ld, u));
   }
-  const float u = __fsub_rn(1.0f, lam_n), l = __fmul_rn(4.0f, ld);  // lambda^4 from 0.77 on
-  float f = 1.0f / 12.0f;
-#pragma unroll
-  for (int k = 11; k >= 2; --k) f = __fmaf_rn(u, f, 1.0f / (float)k);
-  return __fmul_rn(0.25f, __fmaf_rn(__fmul_rn(u, u), f, __fadd_rn(l, u)));
+  return __fmul_rn(0.25f, power_rest(__fmul_rn(4.0f, ld), lam_n));  // lambda^4 from 0.77 on
+}
+
+// What the state before segment q still counts for at the start of segment seg, if segment q has no end of an episode: a
+// power of its own, since a product of the segments' powers would add up their roundings.
+__device__ __forceinline__ float segments_keep(const AttnPass& A, float ld, int q, int seg) {
+  return power(ld, (int)((seg - q) * A.seg_len) - (q == 0 && A.first == 0 ? 1 : 0));
 }
 
 template <class T>

@@ -427,6 +427,10 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
     const float ld = A.ld[h];
     const bool flip = A.reverse != 0, tma = A.tma != 0;
     if (tid <= C) pw[tid] = power(ld, tid);
+    if (tid == C + 1) {  // what lambda^128 lost: over many chunks it would show
+      const float whole = power(ld, C);
+      pw[tid] = __fmul_rn(whole, power_rest(__fmul_rn((float)C, ld), whole));
+    }
     if (tid < C) bad[0][tid] = bad[1][tid] = 0;
     if (tid < 16) near[tid] = power(ld, flip ? tid : 15 - tid);  // lambda^distance within 16 columns, from the near end
     if (tid == 0) {
@@ -493,7 +497,7 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
 #pragma unroll
     for (int y = 0; y < HC; ++y) s[y] = 0.0f;
     if (!KEEP && !closes) {
-      // What the segments before this one added, each times what the ones between kept of it, and the state before them.
+      // What the segments before this one added, each times what the ones between keep of it, and the state before them.
       const bool rows = A.s_in && A.sy == 1;
       float w = 1.0f;
       if (seg > 0 || rows) {
@@ -512,7 +516,7 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
         for (int q = seg - 1; q >= 0 && w != 0.0f; --q) {
           const int64_t at_q = (int64_t)bh * A.segs + q;
           add(A.seg_state + at_q * A.da * A.dc);
-          w = __fmul_rn(w, A.seg_keep[at_q]);
+          w = A.seg_keep[at_q] != 0.0f ? segments_keep(A, ld, q, seg) : 0.0f;
         }
         if (rows && w != 0.0f) add(A.s_in + (int64_t)bh * A.da * A.dc);
 #pragma unroll
@@ -660,7 +664,7 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
       }
     };
 
-    float kept = 1.0f;
+    bool cut_once = false;
 #pragma unroll
     for (int k = KEEP ? 1 : 0; k < 3; ++k) gather(0, k, place(k));
     post_ends(0, ends(0));
@@ -803,8 +807,8 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
       // (4) the state, and what the next chunk's first products take
       wait(&done_bar[1], n);
       tcx::fence_after();
-      const float keep = end < 0 ? pw[m - 1 + lead] : 0.0f;
-      kept = __fmul_rn(kept, keep);
+      const float keep = end < 0 ? pw[m - 1 + lead] : 0.0f, rest = m - 1 + lead == C ? pw[C + 1] : 0.0f;
+      cut_once = cut_once || end >= 0;
 #pragma unroll
       for (int y = 0; y < HC; y += 16) {
         uint32_t u[16];
@@ -812,10 +816,12 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
         tcx::tm_wait();
         tcx::reg_fence16(u);
         if (ok && keep != 0.0f) {
-          const Pair kk = pair(keep, keep);
+          const Pair kk = pair(keep, keep), rr = pair(rest, rest);
 #pragma unroll
-          for (int e = 0; e < 16; e += 2)
-            unpair(fma2(kk, pair(s[y + e], s[y + e + 1]), pair(__uint_as_float(u[e]), __uint_as_float(u[e + 1]))), s[y + e], s[y + e + 1]);
+          for (int e = 0; e < 16; e += 2) {
+            const Pair v = pair(s[y + e], s[y + e + 1]);
+            unpair(fma2(kk, v, fma2(rr, v, pair(__uint_as_float(u[e]), __uint_as_float(u[e + 1])))), s[y + e], s[y + e + 1]);
+          }
         } else {
 #pragma unroll
           for (int e = 0; e < 16; ++e) s[y + e] = ok ? __uint_as_float(u[e]) : nan();
@@ -837,7 +843,7 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
       __threadfence();
     } else if (KEEP) {
       write_rows(A.seg_state + ((int64_t)bh * A.segs + seg) * A.da * A.dc, 1.0f);
-      if (tid == 0) A.seg_keep[(int64_t)bh * A.segs + seg] = kept;
+      if (tid == 0) A.seg_keep[(int64_t)bh * A.segs + seg] = cut_once ? 0.0f : power(ld, p1 - p0 - (p0 == 0 && A.first == 0 ? 1 : 0));
     } else if (A.s_out && seg == A.segs - 1) {
       float f = A.reverse ? power(ld, 1) : 1.0f;
       if (!A.reverse && A.done && A.done[b * A.dsb + (A.len - 1) * A.dst] != 0) f = 0.0f;

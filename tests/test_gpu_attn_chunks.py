@@ -176,3 +176,34 @@ def test_large_scores(simx, D, small):
     for n, x in zip(("grad_q", "grad_k", "grad_v"), g):
         _close(_f64(x), ref[n], ref[n + "_size"], "bf16", T, n)
     _state(_f64(g[3]), ref["ds0"], ref["ds0_size"], T, "ds0")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,T,D", [(400, 40000, 16), (160, 20000, 128), (1, 300000, 64), (3, 60001, 32)])
+def test_long_memories(simx, H, T, D, dtype):
+    """A state over hundreds of chunks of steps that add nothing: lambda^T s0 (backward lambda^T ds_last), cut into
+    segments or not.  Each of at most 2400 multiplications rounds every element by 2^-24 of its own, 3e-8 in the
+    mean square, which is 3e-8 * 49 / 16 < 1e-7 of the mean over a state's 256 elements or more; a power of the decay,
+    three times at most, 2^-22 each: below 1e-6.  A factor that is always rounded the same way would add up to 3e-8
+    for each chunk.  In fp32 and one piece the state is multiplied every fourth step, by as little as 1 - 4e-7: a product
+    s - s 7 2^-24 is rounded to a few whole steps of s, by the same part of a step for as long as s stays near where it is, so that
+    these roundings do not cancel, and all T / 4 of 2^-24 count."""
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    zero = torch.zeros((1, 1, 1, D), dtype=dtype, device="cuda").expand(1, T, H, D)
+    ld = -torch.exp(torch.linspace(np.log(1e-7), np.log(8.0 / T), H, device="cuda"))
+    s0 = torch.rand((1, H, D, D), generator=gen, device="cuda") + 0.5
+    last = torch.empty_like(s0)
+    want, tol = torch.exp(T * ld.double()), T / 4 * 2.0 ** -24 if dtype == torch.float32 and H >= 152 else 1e-6
+    o = torch.empty((1, T, H, D), dtype=dtype, device="cuda")
+    simx.decay_attention(zero, zero, zero, o, ld, _ws(simx.decay_attention_workspace_size(1, T, H, H, D, D)), s0=s0, s_last=last)
+
+    def off(x):
+        return ((x.double() / (s0.double() * want[None, :, None, None]) - 1).mean((0, 2, 3))).abs().max().item()
+    assert not o.any() and off(last) <= tol
+    del o
+    if H * T * D > 1 << 28:
+        return
+    last.zero_()
+    g = [torch.empty((1, T, H, D), dtype=dtype, device="cuda") for _ in range(3)]
+    simx.decay_attention_grad(zero, zero, zero, zero, *g, ld, _ws(simx.decay_attention_grad_workspace_size(1, T, H, H, D, D)), ds_last=s0, ds0=last)
+    assert off(last) <= tol
