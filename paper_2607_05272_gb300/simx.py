@@ -836,7 +836,7 @@ def _attention(q, k, v, log_decay, scale, s0, done):
         dsb, dst = done.stride()
     f, state = torch.float32, (b, h, dk, dv)
     return f, state, (b, t, h, dv), dev, (
-        b, t, h, hk, dk, dv, dt, dk ** -0.5 if scale is None else scale, *_heads(q, "q", q, shape, dev),
+        b, t, h, hk, dk, dv, dt, max(dk, 1) ** -0.5 if scale is None else scale, *_heads(q, "q", q, shape, dev),
         *_heads(k, "k", q, (b, t, hk, dk), dev), *_heads(v, "v", q, (b, t, hk, dv), dev)), (
         _flat(log_decay, "log_decay", f, (h,), dev), _flat(s0, "s0", f, state, dev), d, dsb, dst)
 
