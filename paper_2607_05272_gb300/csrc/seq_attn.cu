@@ -19,9 +19,9 @@ namespace {
 
 constexpr int kThreads = 256;
 // Lengths up to which a state is carried from step to step in a block's registers.  256 x 16 heads of 128 in bf16: 1, 4 and 8
-// steps in 95, 209 and 375 us, 9 by chunks in 380; in fp32 1, 2 and 8 in 100, 135 and 389, by a warp for 16 columns 698,
-// 709 and 739; of 64 in fp32 4 and 8 in 88 and 154, 9 by warps in 131.  1024 x 2 heads of 32 in fp32: 1, 2, 4 and 8
-// steps in 14, 16, 23 and 37 us, by a warp for each head 18.
+// steps in 94, 199 and 359 us, any of them by chunks in 380; in fp32 1, 2 and 8 in 94, 127 and 387, by a warp for 16 columns
+// 714, 724 and 752; of 64 in fp32 4 and 8 in 72 and 123, by warps 123 and 128.  1024 x 2 heads of 32 in fp32: 1, 2, 4 and 8
+// steps in 11, 14, 21 and 31 us, by a warp for each head 14.
 constexpr int kStepMost = 8;
 int most_steps(const simx_attention& a) {
   const int64_t d = std::max(a.dk, a.dv);
@@ -101,7 +101,8 @@ struct Flat {
 // (2 l) on, so that a step is X + X / 8 paired operations a lane without any exchange but the sum of o over g, for four
 // steps at once.  Inputs come by asynchronous copies, a stage ahead; a lane's loads of a and b are the same for eight
 // lanes.  KEEP: only what the segment adds to the state.
-// 1024 sequences of 512 steps, 2 heads of 32: 187 us, 44 % of the copy rate (gradient, three passes: 467 us, 31 %).
+// 1024 sequences of 512 steps, 2 heads of 32: 187 us, 44 % of the copy rate (gradient, three passes: 468 us, 31 %).  Wider
+// heads, 64 sequences: 16 of 64 in 301 us (gradient 777), 8 of 128 in 673 (1841), where HBM would take 85 (148) and 90 (155).
 // Bound by the FP32 units and shared memory's loads, some 65 and 72 us of it alone, with 3.4 warps on a scheduler to
 // cover one another; HBM would take 83.  Tried: two warps or four to a block 198 and 197 us; 16 columns to a warp, for
 // twice the warps, 308; a scale for every step 272; chunks of steps as products of 32 x 32 matrices 355 on the FP32
@@ -461,8 +462,8 @@ struct Plan {
 
 // Long sequences of few heads are cut into segments: their states are found first, for a second read of keys and values.
 // In bf16, heads of all passes that fill the GPU are shared out instead (seq_attn.cuh), each input read once.  16 x 4096 x 16
-// heads of 128: 289 us; in two segments to a head, before that, 670.  4 x 4096 x 16 backward: 227 and 860.  One sequence of 60001, 16 heads
-// of 64, 19 segments: 238, of which the first pass takes some 85.
+// heads of 128: 291 us; in two segments to a head, before that, 670.  4 x 4096 x 16 backward: 247 and 860.  One sequence of
+// 60001, 16 heads of 64, 19 segments: 235, of which the first pass takes 85.
 Plan segments(int64_t segs, int64_t len) {
   int64_t sl = std::max<int64_t>(1, (len + segs - 1) / segs);
   sl = (sl + 127) / 128 * 128;
@@ -470,8 +471,8 @@ Plan segments(int64_t segs, int64_t len) {
 }
 
 // Segments that a length is worth: each costs the later ones a read of its state.  One head of 64, bf16 (fp32): 512 steps in
-// 29 us (100), in two segments 43 (115); 1024 in 43 (182), in four 41 (125), in two 53 (180); 2048 in 74 (344), in eight 41
-// (152), in four 51 (191); 8192 in 250 (1323), in 16 55 (285), in 32 61 (322).
+// 23 us (93), in two segments 27 (96), in four 23 (84); 1024 in 37 (174), in four 29 (117), in two 39 (162); 2048 in 68 (336),
+// in eight 35 (146), in four 39 (182); 8192 in 249 (1309), in 16 41 (181), in 32 33 (146), which the rule gives away.
 int64_t most_segments(int64_t len) { return len < 1024 ? 1 : std::max(len / 512, std::min<int64_t>(len / 256, 8)); }
 
 Plan plan(int dtype, int passes, int64_t batch, int64_t len, int64_t heads, int64_t dk, int64_t dv) {

@@ -69,10 +69,11 @@ struct Passes {
 // passes lie in a row, and each of `grid` blocks takes an equal share of them.  A head that two blocks share is begun by
 // the first before all else; the second takes it up last, from the state in `hand`.  flags: how many blocks have
 // started, then whether each one's state is there.  grid 0: a block for each segment.
-// Dimensions of 128, one block to an SM: 16 x 4096 x 16 heads in 310 us, a block for each head 348; 10 x 2048 x 16 in 120
-// and 188; 64 x 512 x 16 in 222 and 236; where heads come out even, 19 x 2048 x 16, 192 and 193.  Of 64, where one block
-// starts beside another's work anyway: 24 x 2048 x 16 in 157 and 160, backward 8 x 2048 x 16 in 157 and 184, but
-// 40 x 1024 x 16 in 146 and 139 and, backward, 8 x 256 x 16 in 58 and 35.
+// Dimensions of 128, one block to an SM: 16 x 4096 x 16 heads in 291 us, a block for each head 325; 10 x 2048 x 16 in 110
+// and 176; 64 x 512 x 16 in 212 and 219; where heads come out even, 19 x 2048 x 16, 181 and 180; backward 4 x 4096 x 16 in
+// 246 and 334.  Of 64, where one block starts beside another's work anyway: 24 x 2048 x 16 in 133 and 156, backward
+// 8 x 2048 x 16 in 152 and 180, but 8 x 256 x 16 in 41 and 37; the rule's limits (1.5 heads to a block, 2048 steps) give
+// away some: 40 x 1024 x 16 would take 123, by blocks for each head 131.
 struct Shares {
   int grid, per, passes;  // per: chunks of a head
   float* hand;

@@ -176,8 +176,9 @@ struct Maps {
 // cycles at 128 bytes a cycle), and the warps' own reads and writes, the copies in and o out move some 450 KB more (3500),
 // of 9000 cycles that a chunk takes; the tensor cores alone would take 2000.  The rest is the phases above, which all
 // warps go through together: the weighing of b 2000 cycles, o to shared memory 900, scores 1200, the state and its
-// operand 1600.  16 x 4096 x 16 heads of 128: 289 us, 57 % of the copy rate; backward, three passes, 4 x 4096 x 16: 227
-// us, 32 %; one sequence of 60001, 16 heads of 64 on 4: 238 us, 19 %, the length in 19 segments and read twice.
+// operand 1600.  16 x 4096 x 16 heads of 128: 291 us, 57 % of the copy rate; backward, three passes, 4 x 4096 x 16: 247
+// us, 29 %; one sequence of 60001, 16 heads of 64 on 4: 235 us, 20 %, the length in 19 segments and read twice.
+// Backward with 4 heads of keys and values for 16, 4 x 4096: 893 us, most of it the scattered fp32 rows of each head's part.
 //
 // Row r of a chunk's tiles is step r, or in reverse step 127 - r: the copies keep the order of time.
 //
@@ -724,7 +725,7 @@ __global__ void __launch_bounds__(Shape<D>::kThreads + 128, Shape<D>::kBlocks)
       {
         unsigned char* p = sm + place(1) + off0;
         unsigned char* q = sm + S::kMore + off0;
-        // not unrolled: fetching the longer code costs more than it saves (304 us for 16 x 4096 x 16 heads of 128, 297 so)
+        // not unrolled: fetching the longer code costs more than it saves (2 % of 16 x 4096 x 16 heads of 128)
 #pragma unroll 1
         for (int u = 0; u < S::kPieces; ++u, p += kStep * L, q += kStep * L) {
           if (u == S::kPieces / 2) {  // rows up to 63 are done

@@ -15,9 +15,10 @@
 // logit in order-preserving bits above the complement of its index, so that equal logits rank by index and no two
 // keys are equal; each warp keeps its largest in a list, a key to a lane, and one warp merges the lists.
 //
-// Bound by instructions: 8192 rows of 50001 bf16 in 211 us, 58 % of the copy rate, with 21,800 warp instructions to a row
-// (issue 68 % of the time), of which joins, candidates and their ranking are a third; of 131072 in 426 us, 75 %.
-// Logits go in pairs, each with one exponential.  40 registers instead of 48, for more warps, spill: 223 us.
+// Bound by instructions: 8192 rows of 50001 bf16 in 212 us, 58 % of the copy rate, with 22,400 warp instructions to a row
+// (issue 69 % of the time), of which joins, candidates and their ranking are a third; of 131072 in 424 us, 76 %; in fp32
+// 285 and 742 us, 86 %.  Logits go in pairs, each with one exponential.  40 registers instead of 48, for more warps, spill:
+// 223 us.  (A warp to a row of bf16 spills 24 bytes of a thread at 48.)
 #include <algorithm>
 
 #include "kernels.h"
@@ -365,15 +366,16 @@ __global__ void __launch_bounds__(NW == 1 ? 32 * kRows : 32 * NW) k_logprobs(con
 template <class T>
 cudaError_t run(const LogprobArgs& a, cudaStream_t s) {
   count_launches(1);
-  // A warp to a row takes a block's joins off short ones: 8192 rows of 1024, 4096, 16384 logits in 16, 31 and 86 us, by
-  // blocks 109, 76 and 104.  Where rows are long or few, its own reads one after another are what counts: 8192 of 50001
-  // 252 us and 217, 256 of 8192 18 us and 12, and 1024 of 16384 33 us and 25.
+  // A warp to a row takes a block's joins off short ones: 8192 rows of 1024, 4096, 16384 logits of bf16 in 14, 25 and 79 us,
+  // by blocks 103, 68 and 104; of fp32 14, 35 and 140, by blocks 90, 64 and 110, which the rule gives away.  Where rows are
+  // long or few, its own reads one after another are what counts: 8192 of 50001 226 us and 211, 256 of 8192 14 us and 8,
+  // and 1024 of 16384 24 us and 17.
   if (a.V <= 4096 || (a.V <= 16384 && a.V <= 4 * a.n)) {
     k_logprobs<T, 1, false><<<(unsigned)((a.n + kRows - 1) / kRows), 32 * kRows, 0, s>>>(a);
     return cudaGetLastError();
   }
-  // Few rows: the row's stretches of 4096 logits or more to the blocks of a cluster.  16 rows of 131072: 14 us, 31 by a
-  // block each; 128 rows 25 and 33.
+  // Few rows: the row's stretches of 4096 logits or more to the blocks of a cluster.  16 rows of 131072: 10 us, 21 by a
+  // block each; 128 rows 19 and 25.
   unsigned ranks = 1;
   while (ranks < kMostRanks && a.n * ranks < 152 && a.V >= 8192 * (int64_t)ranks) ranks *= 2;
   if (ranks == 1) {

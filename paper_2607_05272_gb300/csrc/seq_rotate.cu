@@ -8,10 +8,12 @@
 // A row is read once (backward: with dy) and written once.  A group of lanes takes a token's heads in turn; a lane
 // holds two units of 16 bytes such that both elements of each of its pairs are its own, so that turning needs no
 // exchange between lanes, and the sines of its pairs, found once per token.  Single elements in place of units where
-// rows lie off that grid: 307 us for what takes 137 on it.
-// 32768 tokens, 32 + 8 heads of 128 in bf16: 134 us, 75 % of the copy rate, bound by HBM at 16 warps an SM (126
-// registers).  Backward, 16384 tokens of 24 + 8 heads of 96: 98 us, 46 %, bound by instructions (350 for the rows of
-// four lane groups of 8, of which two lanes have no unit; two elements at a time, else 100 us) and registers.
+// rows lie off that grid: 301 us for 126 elements where 128 take 134.
+// 32768 tokens, 32 + 8 heads of 128 in bf16: 134 us, 75 % of the copy rate, bound by HBM at 16 warps an SM (119
+// registers); 16384 in fp32 111 us, 90 % (24 bytes of a thread spilled, interleaved 12).  Backward, 16384 tokens of 24 + 8
+// heads of 96: 98 us, 46 %, bound by instructions (350 for the rows of four lane groups of 8, of which two lanes have no
+// unit; two elements at a time, else 100 us) and registers: 72 bytes of a thread are spilled, with halves 92; in fp32 124
+// us, 73 %.
 #include <algorithm>
 
 #include "kernels.h"
@@ -24,7 +26,9 @@ using namespace seq;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostBlocks = 304;  // of the backward pass: each leaves a row of sums
+// Of the backward pass, each of which leaves a row of sums: two to an SM.  152, 304, 608 and 1216 of them: 123, 98, 101 and
+// 107 us for 16384 tokens of 24 + 8 heads of 96, 18, 19, 27 and 39 for 2000 of 8 + 8 of 64.
+constexpr int kMostBlocks = 304;
 
 // One tensor's rows: forward x -> y, backward (x, dy) -> dx.
 struct Side {
