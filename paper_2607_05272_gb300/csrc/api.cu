@@ -1230,7 +1230,7 @@ static bool share_elements(const simx_attention& a, const HeadsOf& x, const Head
   Gap axis[3];
   int n = 0;
   for (const Gap& g : {Gap{x.t->sb, a.batch - 1, a.batch - 1}, Gap{x.t->st, a.len - 1, a.len - 1}, Gap{x.t->sh, y.heads - 1, x.heads - 1}})
-    if (g.stride > 0) axis[n++] = g;
+    if (g.stride > 0 && (g.below || g.above)) axis[n++] = g;
   std::sort(axis, axis + n, [](const Gap& p, const Gap& q) { return p.stride > q.stride; });
   return steps_to(bytes / es, axis, n, y.dim - 1, x.dim - 1);
 }

@@ -96,6 +96,19 @@ def test_what_lies_apart_is_not_refused(lib):
     assert "workspace" in _forward(lib, **kw)
 
 
+def test_axes_of_one(lib):
+    """The stride of an axis that is one long says nothing, whatever it is."""
+    n = 1 << 15
+    for sb in (0, 32, 500, 1 << 30):
+        for sh in (0, 7, 900, 1 << 30):
+            q, k, v = (H(FAKE + i * (1 << 30), sb, 96, sh) for i in range(3))
+            for off in (0, 96, 9600, 96 * (n - 1) + 31, -96 * (n - 1) - 31):
+                kw = dict(batch=1, len=n, heads=1, kv_heads=1, q=q, k=k, v=v)
+                assert _forward(lib, **kw, o=H(k.p + 4 * off, sb, 96, sh)) == "o overlaps k"
+            for off in (32, 64, 96 * n, -96 * n):
+                assert "workspace" in _forward(lib, **kw, o=H(k.p + 4 * off, sb, 96, sh))
+
+
 def test_no_steps(lib):
     """Tensors of no elements share none."""
     x = H(FAKE, 0, 0, 0)
